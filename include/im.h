@@ -553,6 +553,71 @@ im_status im_copy_f32(float *dst, const float *src, int64_t n, void *cuda_stream
 im_status im_colsum_f32(const float *x, int64_t ld, int64_t rows, int32_t cols, float *out, void *workspace,
                         size_t workspace_bytes, void *cuda_stream);
 
+/* ---- layer norm and 8-bit activation checkpoints --------------------------------
+ * (No counterpart in the paper, whose nets are plain MLPs; for policies and critics that normalise their hidden layers, and
+ * for updates whose activations should take a quarter of the memory.)  Building blocks beside the products above, for a
+ * hidden layer Z = H W^T + b (im_gemm_bf16), Y = relu(gamma xh + beta), xh = (Z - mean) rstd.  Everything is asynchronous on
+ * cuda_stream, allocates nothing and is capturable.  x_dtype, y_dtype, ...: IM_DTYPE_F32 or IM_DTYPE_BF16; ld*: row strides in
+ * elements; matrices are row-major; rows that start on 16 bytes are read and written in 16-byte pieces, others element by element
+ * (slower, the same results but for the order of sums).  Columns beyond N are neither read nor written.  All arithmetic and
+ * all sums are fp32 (batch sums are finished in fp64); results are bit-reproducible.  NaN and infinities are carried through.
+ *
+ * im_act8: a matrix in 8 bits.  Columns 32 b .. 32 b + 31 of a row (fewer at its end) share a power of two 2^e, the least
+ * with e >= -100 for which the largest magnitude among them is at most 127 2^e (IM_ACT8_INT8) or 448 2^e (IM_ACT8_E4M3); a code is
+ * value / 2^e rounded to nearest, ties to even, as int8 or as e4m3 (no infinities, 448 the largest).  The scale byte is e + 127;
+ * 255 marks a block with an infinity or a NaN in it: its codes are 0 and every value of it is restored as NaN.
+ *   code   DEVICE [rows][ld_code] bytes      scale  DEVICE [rows][ld_scale] bytes, ld_scale >= ceil(N / 32)
+ * The struct is HOST memory and not kept.  A restored value, code 2^e, is exact in bf16 (what rounded up to
+ * 2^128 or more is restored as an infinity).
+ *
+ * im_layer_norm_forward: per row of x [M][N]:  mean = sum x / N, rstd = 1 / sqrt(sum (x - mean)^2 / N + eps),
+ *   xh = fl32(fl32(x - mean) rstd), y = fl32(gamma xh + beta), with relu != 0 max(y, 0), rounded to y_dtype.
+ *   gamma, beta DEVICE float [N] or NULL (1, 0);  eps > 0;  mean, rstd DEVICE float [M] (written) or NULL;  keep: where
+ *   xh goes in 8 bits, or NULL.  y may be x (same type and stride).  N <= IM_LAYER_NORM_MAX_COLS (IM_ERR_UNSUPPORTED beyond).
+ * im_layer_norm_backward: dy [M][N] the gradient at y.  With h = dy where relu == 0 or fl32(gamma xh + beta) > 0, else 0:
+ *   dx = rstd (gamma h - mean_n(gamma h) - xh mean_n(gamma h xh)),  dgamma = sum_rows h xh,  dbeta = sum_rows h.
+ *   xh comes from x and mean (then it is the forward's, bit for bit, and so is the ReLU's decision) or, with x == NULL, from
+ *   `kept`; exactly one of the two is given.  rstd in either case.  x_dtype: of x and dx.  dx may be dy or x (same type and
+ *   stride) or NULL;  dgamma, dbeta DEVICE float [N], either NULL (not all three).  workspace: DEVICE, 16-byte
+ *   aligned, at least im_layer_norm_workspace_bytes(M, N) (needed for dgamma or dbeta; contents irrelevant; calls that may
+ *   overlap on the GPU need one each).
+ * im_act8_pack / im_act8_unpack: x [M][N] to 8 bits, and back:  out = code 2^e, or with gamma, beta (either may be
+ *   NULL: 1, 0) or relu  fl32(gamma code 2^e + beta), with relu != 0 max(., 0), rounded to out_dtype -- a layer's output from the kept xh.
+ * im_gemm_act8_tn: the weight gradient of the layer above,  C[n][k] = sum_r A[r][n] H[r][k],  n < Mo, k < No, on the
+ *   tensor cores with H restored on the way in: the values im_act8_unpack would give as bf16.  A bf16 [R][lda] (lda a multiple of 8,
+ *   16-byte aligned), C float [Mo][ldc].  H->code 16-byte aligned with ld_code a multiple of 16 and whole rows readable (R ld_code
+ *   bytes).  R, Mo and No need not be multiples of anything; Mo, No <= 65536 (IM_ERR_UNSUPPORTED beyond).  workspace: as
+ *   above, im_gemm_act8_tn_workspace_bytes(R, Mo, No) bytes (which may be 0: then NULL will do).  status DEVICE uint32 [1] receives
+ *   IM_DEV_WAIT_TIMEOUT if a bounded wait inside the kernel runs out. */
+#define IM_DTYPE_F32  0
+#define IM_DTYPE_BF16 1
+#define IM_DTYPE_U32  2
+#define IM_LAYER_NORM_MAX_COLS 8192
+#define IM_ACT8_INT8 0
+#define IM_ACT8_E4M3 1
+typedef struct {
+    uint8_t *code;
+    int64_t ld_code;
+    uint8_t *scale;
+    int64_t ld_scale;
+    int32_t form;                 /* IM_ACT8_* */
+} im_act8;
+im_status im_layer_norm_forward(int32_t M, int32_t N, const void *x, int64_t ldx, int32_t x_dtype, const float *gamma,
+                                const float *beta, float eps, int32_t relu, void *y, int64_t ldy, int32_t y_dtype, float *mean,
+                                float *rstd, const im_act8 *keep, void *cuda_stream);
+size_t im_layer_norm_workspace_bytes(int32_t M, int32_t N);
+im_status im_layer_norm_backward(int32_t M, int32_t N, const void *dy, int64_t ld_dy, int32_t dy_dtype, const void *x,
+                                 int64_t ldx, int32_t x_dtype, const float *mean, const float *rstd, const im_act8 *kept,
+                                 const float *gamma, const float *beta, int32_t relu, void *dx, int64_t ld_dx, float *dgamma,
+                                 float *dbeta, void *workspace, size_t workspace_bytes, void *cuda_stream);
+im_status im_act8_pack(int32_t M, int32_t N, const void *x, int64_t ldx, int32_t x_dtype, const im_act8 *out, void *cuda_stream);
+im_status im_act8_unpack(int32_t M, int32_t N, const im_act8 *in, const float *gamma, const float *beta, int32_t relu, void *out,
+                         int64_t ld_out, int32_t out_dtype, void *cuda_stream);
+size_t im_gemm_act8_tn_workspace_bytes(int32_t R, int32_t Mo, int32_t No);
+im_status im_gemm_act8_tn(const uint16_t *A, int64_t lda, const im_act8 *H, float *C, int64_t ldc, int32_t R, int32_t Mo,
+                          int32_t No, const float *gamma, const float *beta, int32_t relu, void *workspace, size_t workspace_bytes,
+                          uint32_t *status, void *cuda_stream);
+
 /* ---- the update phase as handles ------------------------------------------------
  * (The paper's training loop, Figure 2: `update_policy(storage)` after every rollout; Section 4.1 runs
  * the PPO update as one compiled unit, and Section 4.2 keeps the host out of it.  The hyper-parameter
@@ -600,9 +665,6 @@ typedef struct im_trainer im_trainer;
 #define IM_TRAINER_H       10   /* bf16 [max_rows][Kp]: input of layer l (layer 0: the observations) */
 #define IM_TRAINER_OUT     11   /* float [max_rows][dims[last]]                     */
 #define IM_TRAINER_STATUS  12   /* uint32 [1]: sticky device status word            */
-#define IM_DTYPE_F32  0
-#define IM_DTYPE_BF16 1
-#define IM_DTYPE_U32  2
 im_status im_trainer_create(int32_t n_layers, const int32_t *dims, const float *const *W, const float *const *b,
                             int32_t max_rows, void *cuda_stream, im_trainer **out);
 void im_trainer_destroy(im_trainer *tr);

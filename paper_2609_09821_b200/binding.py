@@ -36,6 +36,8 @@ EXPORTS = [
     "im_ppo_updater_set_step_count",
     "im_copy_f32", "im_gemm_bf16_tn", "im_gather_rows_f32", "im_gemm_bf16_dgrad", "im_env_set_obs_extension", "im_env_adapt_reset_bins", "im_debug_math", "im_debug_set_wait", "im_env_set_summary", "im_clips_set_cyclic",
     "im_env_get_cycles", "im_env_set_cycles", "im_env_set_aos_staging", "im_policy_value_forward",
+    "im_layer_norm_forward", "im_layer_norm_workspace_bytes", "im_layer_norm_backward", "im_act8_pack", "im_act8_unpack",
+    "im_gemm_act8_tn_workspace_bytes", "im_gemm_act8_tn",
 ]
 
 
@@ -100,6 +102,10 @@ class PolicyConfig(C.Structure):
     _fields_ = [("n_layers", C.c_int32), ("dims", C.c_int32 * (MAX_LAYERS + 1)), ("dtype", C.c_int32),
                 ("sigma", C.c_float), ("seed", C.c_uint64), ("env_id_base", C.c_uint32),
                 ("max_batch", C.c_int32), ("impl", C.c_int32)]
+
+
+class Act8View(C.Structure):
+    _fields_ = [("code", C.c_void_p), ("ld_code", C.c_int64), ("scale", C.c_void_p), ("ld_scale", C.c_int64), ("form", C.c_int32)]
 
 
 class ImError(RuntimeError):
@@ -195,8 +201,18 @@ def load():
         L.im_value_forward_staged.argtypes = [vp, vp, i32, vp]
         L.im_policy_value_forward.argtypes = [vp, vp, u32, i32, vp, i32, vp, vp, vp, vp]
         L.im_gae.argtypes = [C.POINTER(GaeConfig), i32, i32, C.c_int64, vp, vp, vp, vp, vp, vp]
+        act8 = C.POINTER(Act8View)
+        L.im_layer_norm_forward.argtypes = [i32, i32, vp, i64, i32, vp, vp, C.c_float, i32, vp, i64, i32, vp, vp, act8, vp]
+        L.im_layer_norm_backward.argtypes = [i32, i32, vp, i64, i32, vp, i64, i32, vp, vp, act8, vp, vp, i32, vp, i64, vp, vp, vp,
+                                             C.c_size_t, vp]
+        L.im_act8_pack.argtypes = [i32, i32, vp, i64, i32, act8, vp]
+        L.im_act8_unpack.argtypes = [i32, i32, act8, vp, vp, i32, vp, i64, i32, vp]
+        L.im_gemm_act8_tn.argtypes = [vp, i64, act8, vp, i64, i32, i32, i32, vp, vp, i32, vp, C.c_size_t, vp, vp]
+        sizes = {"im_layer_norm_workspace_bytes": [i32, i32], "im_gemm_act8_tn_workspace_bytes": [i32, i32, i32]}
+        for name, args in sizes.items():
+            getattr(L, name).argtypes, getattr(L, name).restype = args, C.c_size_t
         for name in EXPORTS:
-            if name not in ("im_status_string", "im_launch_count", "im_ppo_workspace_bytes") \
+            if name not in ("im_status_string", "im_launch_count", "im_ppo_workspace_bytes") and name not in sizes \
                     and not name.startswith("im_destroy") \
                     and name != "im_env_destroy":
                 getattr(L, name).restype = i32
@@ -675,6 +691,147 @@ def colsum(x, out, workspace, stream=None):
     """out[c] = sum over rows of the float32 matrix x."""
     _check(load().im_colsum_f32(_ptr(x), x.stride(0), x.shape[0], x.shape[1], _ptr(out), _ptr(workspace),
                                 workspace.numel() * workspace.element_size(), _st(stream)), "im_colsum_f32")
+
+
+# ---- layer norm and 8-bit activation checkpoints: 2-D CUDA tensors, float32 or bfloat16, row stride = stride(0)
+ACT8_FORMS = {"int8": 0, "e4m3": 1}
+
+
+def _mat(t, what: str, rows: Optional[int] = None, cols: Optional[int] = None, dtypes=("float32", "bfloat16")):
+    """(pointer, row stride, dtype number) of a matrix on the current device, checked against the shape asked for."""
+    if t.dim() != 2 or not t.is_cuda or t.get_device() != _device() or str(t.dtype)[6:] not in dtypes:
+        raise ValueError("%s must be a matrix on the current CUDA device, %s" % (what, " or ".join(dtypes)))
+    m, n = t.shape
+    if (rows is not None and m != rows) or (cols is not None and n != cols) or (n > 1 and t.stride(1) != 1):
+        raise ValueError("%s must be [%s, %s] with adjacent columns" % (what, m if rows is None else rows, n if cols is None else cols))
+    return t.data_ptr(), (t.stride(0) if m > 1 else max(n, 1)), int(t.dtype.itemsize == 2)
+
+
+def _vec(t, n: int, what: str):
+    """Pointer of an optional contiguous float32 vector of n elements on the current device."""
+    if t is None:
+        return None
+    if not t.is_cuda or t.get_device() != _device() or str(t.dtype) != "torch.float32" or t.numel() != n or not t.is_contiguous():
+        raise ValueError("%s must be a contiguous float32 vector of %d elements on the current CUDA device" % (what, n))
+    return t.data_ptr()
+
+
+def _device() -> int:
+    import torch
+    return torch.cuda.current_device()
+
+
+def _scratch(t, what: str):
+    if t is None:
+        return None, 0
+    if not t.is_cuda or t.get_device() != _device() or not t.is_contiguous():
+        raise ValueError("%s must be a contiguous tensor on the current CUDA device" % what)
+    return t.data_ptr(), t.numel() * t.element_size()
+
+
+class Act8:
+    """A [rows, cols] matrix in 8 bits (im_act8): code uint8 [rows, >= cols], scale uint8 [rows, >= ceil(cols / 32)]."""
+
+    def __init__(self, code, scale, cols: int, form: str = "int8"):
+        rows = code.shape[0]
+        pc, lc, _ = _mat(code, "code", dtypes=("uint8",))
+        ps, ls, _ = _mat(scale, "scale", rows=rows, dtypes=("uint8",))
+        if cols < 1 or code.shape[1] < cols or scale.shape[1] < -(-cols // 32):
+            raise ValueError("code and scale are too narrow for %d columns" % cols)
+        if rows == 1:                       # (a lone row's stride is its width)
+            lc, ls = code.shape[1], scale.shape[1]
+        self.code, self.scale, self.rows, self.cols, self.form = code, scale, rows, cols, form
+        self.view = Act8View(pc, lc, ps, ls, ACT8_FORMS[form])
+        self.ref = C.byref(self.view)
+
+    @classmethod
+    def empty(cls, rows: int, cols: int, form: str = "int8"):
+        """Storage for `rows` rows on the current device, laid out as gemm_act8_tn reads it (rows of a multiple of 16 codes)."""
+        import torch
+        new = lambda n: torch.zeros(rows, n, dtype=torch.uint8, device="cuda")  # noqa: E731
+        return cls(new(-(-cols // 16) * 16), new(-(-cols // 32)), cols, form)
+
+
+def _kept(ckpt, rows: int, cols: int):
+    if ckpt is None:
+        return None
+    if ckpt.rows != rows or ckpt.cols != cols or ckpt.code.get_device() != _device():
+        raise ValueError("the checkpoint must be [%d, %d], on the current CUDA device" % (rows, cols))
+    return ckpt.ref
+
+
+def layer_norm(x, gamma, beta, y, mean=None, rstd=None, eps: float = 1e-5, relu: bool = False, ckpt: Optional[Act8] = None, stream=None):
+    """y [M, N] = act(gamma xh + beta), xh the rows of x [M, N] brought to mean 0 and variance 1; the row statistics into
+    mean, rstd [M] and xh in 8 bits into ckpt, where given.  gamma, beta [N] or None; y may be x."""
+    M, N = x.shape
+    px, lx, dx = _mat(x, "x")
+    py, ly, dy = _mat(y, "y", M, N)
+    _check(load().im_layer_norm_forward(M, N, px, lx, dx, _vec(gamma, N, "gamma"), _vec(beta, N, "beta"), eps, int(relu), py, ly, dy,
+                                        _vec(mean, M, "mean"), _vec(rstd, M, "rstd"), _kept(ckpt, M, N), _st(stream)),
+           "im_layer_norm_forward")
+
+
+def layer_norm_workspace(M: int, N: int):
+    """Scratch tensor for layer_norm_backward() on M rows of N columns (or fewer rows)."""
+    import torch
+    return torch.empty(load().im_layer_norm_workspace_bytes(M, N), dtype=torch.uint8, device="cuda")
+
+
+def layer_norm_backward(dy, gamma, beta, rstd, dx, dgamma, dbeta, workspace, relu: bool = False, x=None, mean=None,
+                        ckpt: Optional[Act8] = None, stream=None):
+    """dx [M, N], dgamma, dbeta [N] from dy [M, N], the gradient at layer_norm's y: with x and mean as that call had them, or
+    with its ckpt instead of both.  Any of dx, dgamma and dbeta may be None; dx (float32 if None) has x's type."""
+    M, N = dy.shape
+    pdy, ldy, ddy = _mat(dy, "dy")
+    px = lx = pdx = ldx = None
+    xt = 0
+    if x is not None:
+        px, lx, xt = _mat(x, "x", M, N)
+    if dx is not None:
+        pdx, ldx, dt = _mat(dx, "dx", M, N)
+        if x is not None and dt != xt:
+            raise ValueError("dx must have x's dtype")
+        xt = dt
+    pw, nw = _scratch(workspace, "workspace")
+    _check(load().im_layer_norm_backward(M, N, pdy, ldy, ddy, px, lx or 0, xt, _vec(mean, M, "mean"), _vec(rstd, M, "rstd"),
+                                         _kept(ckpt, M, N), _vec(gamma, N, "gamma"), _vec(beta, N, "beta"), int(relu), pdx, ldx or 0,
+                                         _vec(dgamma, N, "dgamma"), _vec(dbeta, N, "dbeta"), pw, nw, _st(stream)),
+           "im_layer_norm_backward")
+
+
+def act8_pack(x, ckpt: Act8, stream=None):
+    """The matrix x in 8 bits."""
+    M, N = x.shape
+    px, lx, dt = _mat(x, "x")
+    _check(load().im_act8_pack(M, N, px, lx, dt, _kept(ckpt, M, N), _st(stream)), "im_act8_pack")
+
+
+def act8_unpack(ckpt: Act8, out, gamma=None, beta=None, relu: bool = False, stream=None):
+    """out = the values ckpt stands for, or act(gamma v + beta) of them."""
+    M, N = out.shape
+    po, lo, dt = _mat(out, "out")
+    _check(load().im_act8_unpack(M, N, _kept(ckpt, M, N), _vec(gamma, N, "gamma"), _vec(beta, N, "beta"), int(relu), po, lo, dt, _st(stream)),
+           "im_act8_unpack")
+
+
+def gemm_act8_tn_workspace(R: int, Mo: int, No: int):
+    """Scratch tensor for gemm_act8_tn() of these sizes."""
+    import torch
+    return torch.empty(load().im_gemm_act8_tn_workspace_bytes(R, Mo, No), dtype=torch.uint8, device="cuda")
+
+
+def gemm_act8_tn(A, ckpt: Act8, Cout, workspace, status, gamma=None, beta=None, relu: bool = False, stream=None):
+    """Cout [Mo, No] (float32) = A [R, Mo] (bfloat16) transposed times the matrix ckpt [R, No] stands for (act8_unpack's
+    bfloat16 values under gamma, beta, relu)."""
+    R, Mo = A.shape
+    No = ckpt.cols
+    pa, la, _ = _mat(A, "A", dtypes=("bfloat16",))
+    if R == 1:
+        la = -(-Mo // 8) * 8                # (a lone row's stride is free)
+    pc, lc, _ = _mat(Cout, "Cout", Mo, No, dtypes=("float32",))
+    pw, nw = _scratch(workspace, "workspace")
+    _check(load().im_gemm_act8_tn(pa, la, _kept(ckpt, R, No), pc, lc, R, Mo, No, _vec(gamma, No, "gamma"), _vec(beta, No, "beta"),
+                                  int(relu), pw, nw, _ptr(status), _st(stream)), "im_gemm_act8_tn")
 
 
 class _DeviceArray:

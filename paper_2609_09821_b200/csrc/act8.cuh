@@ -1,0 +1,196 @@
+// The 8-bit form of activations (im_act8): 32 consecutive columns of a row share a power of two 2^e, the least with
+// e >= -100 for which the largest magnitude among them fits the code (127 as int8, 448 as e4m3); a code is the value over
+// 2^e, rounded to nearest, ties to even.  A code has at most 7 significant bits, so a restored value is exact in bf16.
+// The scale byte is e + 127 (27 .. 248); 255 marks a block that held an infinity or a NaN and is restored as NaN.
+#pragma once
+#include <cuda_bf16.h>
+#include <cuda_runtime.h>
+#include <stdint.h>
+
+#include "../../include/im.h"
+
+namespace im {
+
+constexpr int kActBlock = 32;
+
+struct Act8View {                          // im_act8 as the kernels take it
+    uint8_t *code, *scale;
+    long long ld_code, ld_scale;
+    int form;                              // IM_ACT8_*
+};
+
+// Whether `a` describes storage for rows of `cols` columns.
+inline bool act8_valid(const im_act8 *a, int cols)
+{
+    return a && a->code && a->scale && (a->form == IM_ACT8_INT8 || a->form == IM_ACT8_E4M3) && a->ld_code >= cols &&
+           a->ld_scale >= (cols + kActBlock - 1) / kActBlock;
+}
+inline Act8View act8_view(const im_act8 *a)
+{
+    Act8View v = {};
+    if (a) { v.code = a->code; v.scale = a->scale; v.ld_code = a->ld_code; v.ld_scale = a->ld_scale; v.form = a->form; }
+    return v;
+}
+
+// Scale byte of a block whose largest |value| has the bits `amax` (as an integer a NaN is larger than infinity, and that
+// larger than any number, so one integer maximum finds both).
+__device__ __forceinline__ uint32_t act8_scale_byte(uint32_t amax, int form)
+{
+    if (amax >= 0x7f800000u) return 255u;
+    const bool i8 = form == IM_ACT8_INT8;
+    // 127 = 1.984375 x 2^6, 448 = 1.75 x 2^8
+    int b = (int)(amax >> 23) - (i8 ? 6 : 8) + ((amax & 0x7fffffu) > (i8 ? 0x7e0000u : 0x600000u) ? 1 : 0);
+    return (uint32_t)(b < 27 ? 27 : b);
+}
+__device__ __forceinline__ float act8_scale(uint32_t byte) { return __uint_as_float(byte == 255u ? 0x7fc00000u : byte << 23); }
+// 1 / 2^e, for byte != 255
+__device__ __forceinline__ float act8_inverse(uint32_t byte) { return __uint_as_float((254u - byte) << 23); }
+
+__device__ __forceinline__ uint32_t abs_bits(float x) { return __float_as_uint(x) & 0x7fffffffu; }
+
+// Codes of four values already divided by 2^e (zeros for a block marked 255), lowest byte first.
+__device__ __forceinline__ uint32_t act8_encode4(float a, float b, float c, float d, int form)
+{
+    if (form == IM_ACT8_INT8) {
+        // 1.5 x 2^23 + v: the sum's low byte is the integer nearest to v, in two's complement
+        const uint32_t p = __float_as_uint(a + 12582912.0f), q = __float_as_uint(b + 12582912.0f);
+        const uint32_t r = __float_as_uint(c + 12582912.0f), s = __float_as_uint(d + 12582912.0f);
+        return __byte_perm(__byte_perm(p, q, 0x0040), __byte_perm(r, s, 0x0040), 0x5410);
+    }
+    uint16_t lo, hi;
+    asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(lo) : "f"(b), "f"(a));
+    asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(hi) : "f"(d), "f"(c));
+    return (uint32_t)lo | ((uint32_t)hi << 16);
+}
+// The numbers that four codes stand for, without their scale.
+__device__ __forceinline__ void act8_decode4(uint32_t w, int form, float (&v)[4])
+{
+    if (form == IM_ACT8_INT8) {
+        // 2^23 + (code + 128) by its bits, minus 2^23 + 128: exact
+        const uint32_t u = w ^ 0x80808080u;
+        v[0] = __uint_as_float(__byte_perm(u, 0x4b000000u, 0x7440)) - 8388736.0f;
+        v[1] = __uint_as_float(__byte_perm(u, 0x4b000000u, 0x7441)) - 8388736.0f;
+        v[2] = __uint_as_float(__byte_perm(u, 0x4b000000u, 0x7442)) - 8388736.0f;
+        v[3] = __uint_as_float(__byte_perm(u, 0x4b000000u, 0x7443)) - 8388736.0f;
+        return;
+    }
+    uint32_t h[2];
+    asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(h[0]) : "h"((uint16_t)(w & 0xffffu)));
+    asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(h[1]) : "h"((uint16_t)(w >> 16)));
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+        asm("{\n\t.reg .b16 l, u;\n\tmov.b32 {l, u}, %2;\n\tcvt.f32.f16 %0, l;\n\tcvt.f32.f16 %1, u;\n\t}" : "=f"(v[2 * i]), "=f"(v[2 * i + 1]) : "r"(h[i]));
+}
+
+// ------------------------------------------------------------------ rows of fp32 or bf16 values
+// A thread's eight values of a row: VEC: eight neighbours, column col .. col + 7, by 16-byte accesses (the row's start allows
+// them; a group that crosses the row's end goes element by element); else columns col, col + step, .. .
+// Loads go past L1 for good (.cs) and are coherent: outputs may lie where inputs lie.
+template <typename T> struct Eight;
+template <> struct Eight<float> { float4 a, b; };
+template <> struct Eight<__nv_bfloat16> { uint4 a; };
+
+__device__ __forceinline__ float to_float(float x) { return x; }
+__device__ __forceinline__ float to_float(__nv_bfloat16 x) { return __bfloat162float(x); }
+__device__ __forceinline__ void store_as(float *p, float x) { *p = x; }
+__device__ __forceinline__ void store_as(__nv_bfloat16 *p, float x) { *p = __float2bfloat16_rn(x); }
+
+__device__ __forceinline__ void set_element(Eight<float> &e, int j, float x) { reinterpret_cast<float *>(&e)[j] = x; }
+__device__ __forceinline__ void set_element(Eight<__nv_bfloat16> &e, int j, __nv_bfloat16 x) { reinterpret_cast<__nv_bfloat16 *>(&e)[j] = x; }
+__device__ __forceinline__ Eight<float> zero8(const float *) { return {make_float4(0.f, 0.f, 0.f, 0.f), make_float4(0.f, 0.f, 0.f, 0.f)}; }
+__device__ __forceinline__ Eight<__nv_bfloat16> zero8(const __nv_bfloat16 *) { return {make_uint4(0u, 0u, 0u, 0u)}; }
+__device__ __forceinline__ Eight<float> full8(const float *p)
+{
+    return {__ldcs(reinterpret_cast<const float4 *>(p)), __ldcs(reinterpret_cast<const float4 *>(p) + 1)};
+}
+__device__ __forceinline__ Eight<__nv_bfloat16> full8(const __nv_bfloat16 *p) { return {__ldcs(reinterpret_cast<const uint4 *>(p))}; }
+
+template <bool VEC, typename T>
+__device__ __forceinline__ Eight<T> load8(const T *row, int col, int step, int cols)
+{
+    if (VEC && col + 8 <= cols) return full8(row + col);
+    Eight<T> e = zero8(row);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        const int c = VEC ? col + j : col + j * step;
+        if (c < cols) set_element(e, j, row[c]);
+    }
+    return e;
+}
+__device__ __forceinline__ void unpack8(const Eight<float> &e, float *v)
+{
+    v[0] = e.a.x; v[1] = e.a.y; v[2] = e.a.z; v[3] = e.a.w;
+    v[4] = e.b.x; v[5] = e.b.y; v[6] = e.b.z; v[7] = e.b.w;
+}
+__device__ __forceinline__ void unpack8(const Eight<__nv_bfloat16> &e, float *v)
+{
+    const uint32_t w[4] = {e.a.x, e.a.y, e.a.z, e.a.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        v[2 * i] = __uint_as_float(w[i] << 16);
+        v[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+    }
+}
+__device__ __forceinline__ void full_store8(float *p, const float *v)
+{
+    reinterpret_cast<float4 *>(p)[0] = make_float4(v[0], v[1], v[2], v[3]);
+    reinterpret_cast<float4 *>(p)[1] = make_float4(v[4], v[5], v[6], v[7]);
+}
+__device__ __forceinline__ void full_store8(__nv_bfloat16 *p, const float *v)
+{
+    uint32_t w[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const __nv_bfloat162 h = __floats2bfloat162_rn(v[2 * i], v[2 * i + 1]);
+        w[i] = *reinterpret_cast<const uint32_t *>(&h);
+    }
+    *reinterpret_cast<uint4 *>(p) = make_uint4(w[0], w[1], w[2], w[3]);
+}
+template <bool VEC, typename T>
+__device__ __forceinline__ void store8(T *row, int col, int step, int cols, const float *v)
+{
+    if (VEC && col + 8 <= cols) {
+        full_store8(row + col, v);
+        return;
+    }
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        const int c = VEC ? col + j : col + j * step;
+        if (c < cols) store_as(row + c, v[j]);
+    }
+}
+// Eight codes of a row, in the same two arrangements.
+template <bool VEC>
+__device__ __forceinline__ uint2 load_codes8(const uint8_t *row, int col, int step, int cols)
+{
+    if (VEC && col + 8 <= cols) return __ldcs(reinterpret_cast<const uint2 *>(row + col));
+    uint32_t w[2] = {0u, 0u};
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        const int c = VEC ? col + j : col + j * step;
+        if (c < cols) w[j >> 2] |= (uint32_t)row[c] << (8 * (j & 3));
+    }
+    return make_uint2(w[0], w[1]);
+}
+template <bool VEC>
+__device__ __forceinline__ void store_codes8(uint8_t *row, int col, int step, int cols, uint2 w)
+{
+    if (VEC && col + 8 <= cols) {
+        *reinterpret_cast<uint2 *>(row + col) = w;
+        return;
+    }
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        const int c = VEC ? col + j : col + j * step;
+        if (c < cols) row[c] = (uint8_t)((j < 4 ? w.x : w.y) >> (8 * (j & 3)));
+    }
+}
+
+inline bool aligned_to(const void *p, uintptr_t bytes) { return (reinterpret_cast<uintptr_t>(p) & (bytes - 1)) == 0; }
+inline size_t dtype_size(int dtype) { return dtype == IM_DTYPE_F32 ? 4 : 2; }
+inline bool float_dtype(int dtype) { return dtype == IM_DTYPE_F32 || dtype == IM_DTYPE_BF16; }
+// Whether every row of [.][ld] starts on 16 bytes.
+inline bool rows_aligned16(const void *p, int64_t ld, int dtype) { return aligned_to(p, 16) && (ld * (int64_t)dtype_size(dtype)) % 16 == 0; }
+inline bool codes_aligned8(const Act8View &v) { return aligned_to(v.code, 8) && v.ld_code % 8 == 0; }
+
+}  // namespace im

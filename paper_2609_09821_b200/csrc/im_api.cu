@@ -846,6 +846,7 @@ im_status im_debug_set_wait(uint64_t limit_ns, int32_t skip_loads)
     if (limit_ns == 0) return IM_ERR_INVALID_ARG;
     IM_CUDA(cudaDeviceSynchronize());                   // kernels in flight keep the setting they started with
     IM_CUDA(tc_set_wait_debug(limit_ns, skip_loads != 0));
+    IM_CUDA(act8_set_wait_debug(limit_ns, skip_loads != 0));
     IM_CUDA(ppo_set_wait_debug(limit_ns, skip_loads != 0));
     return IM_OK;
 }

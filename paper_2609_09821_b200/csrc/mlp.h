@@ -64,6 +64,7 @@ im_status tc_gemm_tn(const GemmOperands &x, const GemmOperands *y, int R, int Mo
 im_status tc_gemm_head(const GemmOperands &x, const GemmOperands *y, int M, int N, int N2, int K, uint32_t *status, uint32_t *status2,
                        cudaStream_t stream);
 // bounded-wait diagnostics of the tensor-core GEMM kernels and of the bulk-copy PPO loss kernel (current device)
+cudaError_t act8_set_wait_debug(unsigned long long limit_ns, int skip_loads);
 cudaError_t tc_set_wait_debug(unsigned long long limit_ns, int skip_loads);
 cudaError_t ppo_set_wait_debug(unsigned long long limit_ns, int skip_loads);
 }  // namespace im

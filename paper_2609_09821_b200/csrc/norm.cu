@@ -1,0 +1,245 @@
+// Layer norm of activation rows, forward, and the entry points of both passes.
+//
+//   mean = sum x / N,  rstd = 1 / sqrt(sum (x - mean)^2 / N + eps),  xh = (x - mean) rstd,  y = act(gamma xh + beta)
+//
+// A row is read once: it stays in the registers of 8 to 256 threads while its mean and then the squares about that mean are
+// summed (two passes over registers, so an offset much larger than the spread costs no digits), fp32 throughout.
+// What bounds it is HBM: every byte of x and y moves once.
+#include <cmath>
+
+#include "im_internal.h"
+#include "norm.h"
+
+namespace im {
+
+namespace {
+
+constexpr int kThreads = 256;
+
+template <int T>
+__device__ __forceinline__ float row_sum(float v, float *shared)
+{
+#pragma unroll
+    for (int o = (T < 32 ? T : 32) / 2; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+    if (T > 32) {
+        if ((threadIdx.x & 31) == 0) shared[threadIdx.x >> 5] = v;
+        __syncthreads();
+        v = 0.0f;
+#pragma unroll
+        for (int w = 0; w < T / 32; ++w) v += shared[w];
+    }
+    return v;
+}
+
+// T threads share a row, each holding C groups of eight values: VEC neighbours, else every T-th column.
+template <typename TX, typename TY, bool VEC, int T, int C>
+__global__ void __launch_bounds__(kThreads) norm_forward_kernel(const NormForward P)
+{
+    constexpr int kGroups = kThreads / T;                         // rows of a CTA at a time
+    __shared__ float s_sum[2][kThreads / 32];
+    const int t = threadIdx.x & (T - 1), g = threadIdx.x / T, N = P.N;
+    const TX *x = static_cast<const TX *>(P.x);
+    TY *y = static_cast<TY *>(P.y);
+    const auto first = [&](int c) { return VEC ? (c * T + t) * 8 : c * 8 * T + t; };
+    const float n = (float)N;
+
+    Eight<TX> raw[C];
+    const auto load_row = [&](long long r) {
+#pragma unroll
+        for (int c = 0; c < C; ++c) raw[c] = r < P.M ? load8<VEC>(x + r * P.ldx, first(c), T, N) : zero8(x);
+    };
+    const long long step = (long long)gridDim.x * kGroups;
+    load_row((long long)blockIdx.x * kGroups + g);
+    for (long long base = (long long)blockIdx.x * kGroups; base < P.M; base += step) {       // (the whole CTA together)
+        const long long r = base + g;
+        float v[8 * C];
+#pragma unroll
+        for (int c = 0; c < C; ++c) unpack8(raw[c], v + 8 * c);
+        if (base + step < P.M) load_row(r + step);
+        float s = 0.0f;
+#pragma unroll
+        for (int i = 0; i < 8 * C; ++i) s += v[i];
+        const float mean = row_sum<T>(s, s_sum[0]) / n;
+        s = 0.0f;
+#pragma unroll
+        for (int c = 0; c < C; ++c)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const float d = __fsub_rn(v[8 * c + j], mean);
+                v[8 * c + j] = d;
+                if (VEC ? first(c) + j < N : first(c) + j * T < N) s = fmaf(d, d, s);
+            }
+        const float rstd = 1.0f / sqrtf(row_sum<T>(s, s_sum[1]) / n + P.eps);
+        if (r < P.M && t == 0) {
+            if (P.mean) P.mean[r] = mean;
+            if (P.rstd) P.rstd[r] = rstd;
+        }
+#pragma unroll
+        for (int c = 0; c < C; ++c) {
+            const int col = first(c);
+            float *e = v + 8 * c;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) e[j] = __fmul_rn(e[j], rstd);     // xh, by the operations that the backward pass repeats
+            if (P.keep.code) {
+                const auto in_row = [&](int j) { return VEC ? col + j < N : col + j * T < N; };
+                if (VEC) {
+                    uint32_t amax = 0u;
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) amax = max(amax, in_row(j) ? abs_bits(e[j]) : 0u);
+                    amax = max(amax, __shfl_xor_sync(0xffffffffu, amax, 1));
+                    amax = max(amax, __shfl_xor_sync(0xffffffffu, amax, 2));
+                    const uint32_t byte = act8_scale_byte(amax, P.keep.form);
+                    const float inv = byte == 255u ? 0.0f : act8_inverse(byte);
+                    float q[8];
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) q[j] = byte == 255u ? 0.0f : e[j] * inv;
+                    if (r < P.M && col < N) {
+                        store_codes8<true>(P.keep.code + r * P.keep.ld_code, col, T, N,
+                                           make_uint2(act8_encode4(q[0], q[1], q[2], q[3], P.keep.form), act8_encode4(q[4], q[5], q[6], q[7], P.keep.form)));
+                        if ((t & 3) == 0) P.keep.scale[r * P.keep.ld_scale + (col >> 5)] = (uint8_t)byte;
+                    }
+                } else {
+                    // the 32 columns of a block are a warp's 32 lanes at one j
+                    uint32_t w[2] = {0u, 0u};
+                    float q[8];
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) {
+                        const uint32_t amax = __reduce_max_sync(0xffffffffu, in_row(j) ? abs_bits(e[j]) : 0u);
+                        const uint32_t byte = act8_scale_byte(amax, P.keep.form);
+                        q[j] = byte == 255u ? 0.0f : e[j] * act8_inverse(byte);
+                        if ((threadIdx.x & 31) == 0 && r < P.M && in_row(j)) P.keep.scale[r * P.keep.ld_scale + ((col + j * T) >> 5)] = (uint8_t)byte;
+                    }
+                    w[0] = act8_encode4(q[0], q[1], q[2], q[3], P.keep.form);
+                    w[1] = act8_encode4(q[4], q[5], q[6], q[7], P.keep.form);
+                    if (r < P.M) store_codes8<false>(P.keep.code + r * P.keep.ld_code, col, T, N, make_uint2(w[0], w[1]));
+                }
+            }
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const int k = VEC ? col + j : col + j * T;
+                const float ga = P.gamma && k < N ? __ldg(P.gamma + k) : 1.0f, be = P.beta && k < N ? __ldg(P.beta + k) : 0.0f;
+                e[j] = __fmaf_rn(ga, e[j], be);
+                if (P.relu) e[j] = e[j] < 0.0f ? 0.0f : e[j];              // (a NaN stays)
+            }
+            if (r < P.M) store8<VEC>(y + r * P.ldy, col, T, N, e);
+        }
+    }
+}
+
+// Column sums of the backward pass: the partial rows in fp64, sixteen threads a column, added in a fixed order.
+constexpr int kFinishParts = 16;
+__global__ void __launch_bounds__(32 * kFinishParts) norm_finish_kernel(const float *partial, int n_partials, int N, float *dgamma, float *dbeta)
+{
+    __shared__ double part[kFinishParts][33];
+    const int c = blockIdx.x * 32 + threadIdx.x;                          // of [dgamma | dbeta]
+    double s = 0.0;
+    if (c < 2 * N)
+        for (int i = threadIdx.y; i < n_partials; i += kFinishParts) s += (double)partial[(long long)i * 2 * N + c];
+    part[threadIdx.y][threadIdx.x] = s;
+    __syncthreads();
+    if (threadIdx.y == 0 && c < 2 * N) {
+        double sum = 0.0;
+#pragma unroll
+        for (int p = 0; p < kFinishParts; ++p) sum += part[p][threadIdx.x];
+        float *out = c < N ? dgamma : dbeta;
+        if (out) out[c < N ? c : c - N] = (float)sum;
+    }
+}
+
+template <typename TX, typename TY, bool VEC, int T, int C>
+cudaError_t launch_forward(const NormForward &a, int n_sm, cudaStream_t stream)
+{
+    constexpr int kGroups = kThreads / T;
+    const long long want = ((long long)a.M + kGroups - 1) / kGroups, most = (long long)n_sm * 8;
+    norm_forward_kernel<TX, TY, VEC, T, C><<<(unsigned)(want < most ? want : most), kThreads, 0, stream>>>(a);
+    return cudaGetLastError();
+}
+template <typename TX, typename TY>
+cudaError_t dispatch_forward(const NormForward &a, bool vec, int n_sm, cudaStream_t st)
+{
+    const int N = a.N;
+    if (!vec) {
+        if (N <= 256) return launch_forward<TX, TY, false, 32, 1>(a, n_sm, st);
+        if (N <= 1024) return launch_forward<TX, TY, false, 32, 4>(a, n_sm, st);
+        return launch_forward<TX, TY, false, 256, 4>(a, n_sm, st);
+    }
+    if (N <= 64) return launch_forward<TX, TY, true, 8, 1>(a, n_sm, st);
+    if (N <= 128) return launch_forward<TX, TY, true, 16, 1>(a, n_sm, st);
+    if (N <= 256) return launch_forward<TX, TY, true, 32, 1>(a, n_sm, st);
+    if (N <= 512) return launch_forward<TX, TY, true, 32, 2>(a, n_sm, st);
+    if (N <= 1024) return launch_forward<TX, TY, true, 32, 4>(a, n_sm, st);
+    if (N <= 2048) return launch_forward<TX, TY, true, 256, 1>(a, n_sm, st);
+    if (N <= 4096) return launch_forward<TX, TY, true, 256, 2>(a, n_sm, st);
+    return launch_forward<TX, TY, true, 256, 4>(a, n_sm, st);
+}
+
+}  // namespace
+
+cudaError_t launch_norm_forward(const NormForward &a, int x_dtype, int y_dtype, int n_sm, cudaStream_t stream)
+{
+    const bool vec = rows_aligned16(a.x, a.ldx, x_dtype) && rows_aligned16(a.y, a.ldy, y_dtype) && (!a.keep.code || codes_aligned8(a.keep));
+    if (x_dtype == IM_DTYPE_F32)
+        return y_dtype == IM_DTYPE_F32 ? dispatch_forward<float, float>(a, vec, n_sm, stream) : dispatch_forward<float, __nv_bfloat16>(a, vec, n_sm, stream);
+    return y_dtype == IM_DTYPE_F32 ? dispatch_forward<__nv_bfloat16, float>(a, vec, n_sm, stream)
+                                   : dispatch_forward<__nv_bfloat16, __nv_bfloat16>(a, vec, n_sm, stream);
+}
+
+}  // namespace im
+
+extern "C" {
+
+im_status im_layer_norm_forward(int32_t M, int32_t N, const void *x, int64_t ldx, int32_t x_dtype, const float *gamma, const float *beta, float eps,
+                                int32_t relu, void *y, int64_t ldy, int32_t y_dtype, float *mean, float *rstd, const im_act8 *keep, void *cuda_stream)
+{
+    using namespace im;
+    if (!x || !y || M < 1 || N < 1 || ldx < N || ldy < N || !float_dtype(x_dtype) || !float_dtype(y_dtype) || !(eps > 0.0f) || std::isinf(eps)) return IM_ERR_INVALID_ARG;
+    if (!aligned_to(x, dtype_size(x_dtype)) || !aligned_to(y, dtype_size(y_dtype))) return IM_ERR_INVALID_ARG;
+    if (keep && !act8_valid(keep, N)) return IM_ERR_INVALID_ARG;
+    if (N > kNormMaxCols) return IM_ERR_UNSUPPORTED;
+    const int n_sm = device_sm_count();
+    if (n_sm <= 0) return IM_ERR_UNSUPPORTED;
+    NormForward a;
+    a.x = x; a.y = y; a.ldx = ldx; a.ldy = ldy; a.M = M; a.N = N; a.relu = relu != 0;
+    a.gamma = gamma; a.beta = beta; a.eps = eps; a.mean = mean; a.rstd = rstd; a.keep = act8_view(keep);
+    const cudaError_t e = launch_norm_forward(a, x_dtype, y_dtype, n_sm, (cudaStream_t)cuda_stream);
+    g_launches.fetch_add(1, std::memory_order_relaxed);
+    return e == cudaSuccess ? IM_OK : IM_ERR_CUDA;
+}
+
+size_t im_layer_norm_workspace_bytes(int32_t M, int32_t N)
+{
+    using namespace im;
+    if (M < 1 || N < 1) return 0;
+    return (size_t)(M < kNormMaxPartials ? M : kNormMaxPartials) * 2 * (size_t)N * sizeof(float);
+}
+
+im_status im_layer_norm_backward(int32_t M, int32_t N, const void *dy, int64_t ld_dy, int32_t dy_dtype, const void *x, int64_t ldx, int32_t x_dtype,
+                                 const float *mean, const float *rstd, const im_act8 *kept, const float *gamma, const float *beta, int32_t relu, void *dx,
+                                 int64_t ld_dx, float *dgamma, float *dbeta, void *workspace, size_t workspace_bytes, void *cuda_stream)
+{
+    using namespace im;
+    const bool sums = dgamma || dbeta;
+    if (!dy || !rstd || M < 1 || N < 1 || ld_dy < N || !float_dtype(x_dtype) || !float_dtype(dy_dtype) || (!dx && !sums)) return IM_ERR_INVALID_ARG;
+    if (!x == !kept || (x && (!mean || ldx < N)) || (kept && !act8_valid(kept, N)) || (dx && ld_dx < N)) return IM_ERR_INVALID_ARG;
+    if (!aligned_to(dy, dtype_size(dy_dtype)) || !aligned_to(x, dtype_size(x_dtype)) || !aligned_to(dx, dtype_size(x_dtype))) return IM_ERR_INVALID_ARG;
+    if (sums && (!workspace || !aligned_to(workspace, 16) || workspace_bytes < im_layer_norm_workspace_bytes(M, N))) return IM_ERR_INVALID_ARG;
+    if (N > kNormMaxCols) return IM_ERR_UNSUPPORTED;
+    const int n_sm = device_sm_count();
+    if (n_sm <= 0) return IM_ERR_UNSUPPORTED;
+    NormBackward a;
+    a.dy = dy; a.x = x; a.dx = dx; a.ld_dy = ld_dy; a.ldx = ldx; a.ld_dx = ld_dx; a.M = M; a.N = N; a.relu = relu != 0;
+    a.mean = mean; a.rstd = rstd; a.gamma = gamma; a.beta = beta; a.kept = act8_view(kept);
+    a.partial = sums ? static_cast<float *>(workspace) : nullptr;
+    int n_partials = 0;
+    cudaStream_t st = (cudaStream_t)cuda_stream;
+    cudaError_t e = launch_norm_backward(a, x_dtype, dy_dtype, n_sm, &n_partials, st);
+    g_launches.fetch_add(1, std::memory_order_relaxed);
+    if (e == cudaSuccess && sums) {
+        norm_finish_kernel<<<(2 * N + 31) / 32, dim3(32, kFinishParts), 0, st>>>(a.partial, n_partials, N, dgamma, dbeta);
+        g_launches.fetch_add(1, std::memory_order_relaxed);
+        e = cudaGetLastError();
+    }
+    return e == cudaSuccess ? IM_OK : IM_ERR_CUDA;
+}
+
+}  // extern "C"

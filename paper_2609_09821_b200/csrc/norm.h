@@ -1,0 +1,37 @@
+// Layer norm kernels: arguments and launchers.
+#pragma once
+#include <cuda_runtime.h>
+#include <stdint.h>
+
+#include "act8.cuh"
+
+namespace im {
+
+constexpr int kNormMaxCols = 8192;
+constexpr int kNormMaxPartials = 592;      // rows of partial column sums that the backward pass leaves at most: four CTAs on each of 148 SMs
+
+struct NormForward {
+    const void *x;
+    void *y;
+    long long ldx, ldy;
+    int M, N, relu;
+    const float *gamma, *beta;             // or null: 1, 0
+    float eps;
+    float *mean, *rstd;                    // [M] or null
+    Act8View keep;                         // code null: nothing is kept
+};
+struct NormBackward {
+    const void *dy, *x;                    // x null: the normalised values come from `kept`
+    void *dx;                              // or null
+    long long ld_dy, ldx, ld_dx;
+    int M, N, relu;
+    const float *mean, *rstd, *gamma, *beta;
+    Act8View kept;
+    float *partial;                        // [gridDim.x][2][N] column sums of h xh and of h, or null
+};
+
+cudaError_t launch_norm_forward(const NormForward &a, int x_dtype, int y_dtype, int n_sm, cudaStream_t stream);
+// *n_partials: the rows of a.partial written
+cudaError_t launch_norm_backward(const NormBackward &a, int x_dtype, int dy_dtype, int n_sm, int *n_partials, cudaStream_t stream);
+
+}  // namespace im
