@@ -32,6 +32,46 @@ inline Act8View act8_view(const im_act8 *a)
     return v;
 }
 
+// ------------------------------------------------------------------ two fp32 values in one register pair
+// Each operation rounds both halves as its scalar form does; the packed forms take one issue slot for two results.
+struct F2 { unsigned long long v; };
+__device__ __forceinline__ F2 f2(float lo, float hi)
+{
+    F2 r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r.v) : "f"(lo), "f"(hi));
+    return r;
+}
+__device__ __forceinline__ F2 f2(float x) { return f2(x, x); }
+__device__ __forceinline__ float lo(F2 a) { return __uint_as_float((uint32_t)a.v); }
+__device__ __forceinline__ float hi(F2 a) { return __uint_as_float((uint32_t)(a.v >> 32)); }
+__device__ __forceinline__ F2 add2(F2 a, F2 b)
+{
+    F2 r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v));
+    return r;
+}
+__device__ __forceinline__ F2 mul2(F2 a, F2 b)
+{
+    F2 r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v));
+    return r;
+}
+__device__ __forceinline__ F2 fma2(F2 a, F2 b, F2 c)
+{
+    F2 r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r.v) : "l"(a.v), "l"(b.v), "l"(c.v));
+    return r;
+}
+// bf16 of both halves, the low one in the low bits; RELU: negative values become 0, a NaN stays one.
+template <bool RELU>
+__device__ __forceinline__ uint32_t bf16x2(F2 a)
+{
+    uint32_t r;
+    if (RELU) asm("cvt.rn.relu.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi(a)), "f"(lo(a)));
+    else asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi(a)), "f"(lo(a)));
+    return r;
+}
+
 // Scale byte of a block whose largest |value| has the bits `amax` (as an integer a NaN is larger than infinity, and that
 // larger than any number, so one integer maximum finds both).
 __device__ __forceinline__ uint32_t act8_scale_byte(uint32_t amax, int form)
@@ -63,23 +103,33 @@ __device__ __forceinline__ uint32_t act8_encode4(float a, float b, float c, floa
     return (uint32_t)lo | ((uint32_t)hi << 16);
 }
 // The numbers that four codes stand for, without their scale.
-__device__ __forceinline__ void act8_decode4(uint32_t w, int form, float (&v)[4])
+template <int FORM>
+__device__ __forceinline__ void act8_decode4(uint32_t w, F2 &a, F2 &b)
 {
-    if (form == IM_ACT8_INT8) {
+    if (FORM == IM_ACT8_INT8) {
         // 2^23 + (code + 128) by its bits, minus 2^23 + 128: exact
         const uint32_t u = w ^ 0x80808080u;
-        v[0] = __uint_as_float(__byte_perm(u, 0x4b000000u, 0x7440)) - 8388736.0f;
-        v[1] = __uint_as_float(__byte_perm(u, 0x4b000000u, 0x7441)) - 8388736.0f;
-        v[2] = __uint_as_float(__byte_perm(u, 0x4b000000u, 0x7442)) - 8388736.0f;
-        v[3] = __uint_as_float(__byte_perm(u, 0x4b000000u, 0x7443)) - 8388736.0f;
+        const F2 off = f2(-8388736.0f);
+        a = add2(f2(__uint_as_float(__byte_perm(u, 0x4b000000u, 0x7440)), __uint_as_float(__byte_perm(u, 0x4b000000u, 0x7441))), off);
+        b = add2(f2(__uint_as_float(__byte_perm(u, 0x4b000000u, 0x7442)), __uint_as_float(__byte_perm(u, 0x4b000000u, 0x7443))), off);
         return;
     }
-    uint32_t h[2];
-    asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(h[0]) : "h"((uint16_t)(w & 0xffffu)));
-    asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(h[1]) : "h"((uint16_t)(w >> 16)));
+    float v[4];
 #pragma unroll
-    for (int i = 0; i < 2; ++i)
-        asm("{\n\t.reg .b16 l, u;\n\tmov.b32 {l, u}, %2;\n\tcvt.f32.f16 %0, l;\n\tcvt.f32.f16 %1, u;\n\t}" : "=f"(v[2 * i]), "=f"(v[2 * i + 1]) : "r"(h[i]));
+    for (int i = 0; i < 2; ++i) {
+        uint32_t h;
+        asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(h) : "h"((uint16_t)(w >> (16 * i))));
+        asm("{\n\t.reg .b16 l, u;\n\tmov.b32 {l, u}, %2;\n\tcvt.f32.f16 %0, l;\n\tcvt.f32.f16 %1, u;\n\t}" : "=f"(v[2 * i]), "=f"(v[2 * i + 1]) : "r"(h));
+    }
+    a = f2(v[0], v[1]);
+    b = f2(v[2], v[3]);
+}
+__device__ __forceinline__ void act8_decode4(uint32_t w, int form, float (&v)[4])
+{
+    F2 a, b;
+    if (form == IM_ACT8_INT8) act8_decode4<IM_ACT8_INT8>(w, a, b);
+    else act8_decode4<IM_ACT8_E4M3>(w, a, b);
+    v[0] = lo(a); v[1] = hi(a); v[2] = lo(b); v[3] = hi(b);
 }
 
 // ------------------------------------------------------------------ rows of fp32 or bf16 values

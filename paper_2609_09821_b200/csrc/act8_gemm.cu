@@ -1,18 +1,24 @@
 // Weight gradient from an 8-bit checkpoint: C[n][k] = sum over rows r of A[r][n] H[r][k], A bf16 (the gradient at a layer's
 // pre-activation), H restored from im_act8: code 2^e, or bf16(act(gamma code 2^e + beta)).  fp32 accumulation and output.
 //
-// One CTA per SM: warp 0 fetches A's tiles by TMA (64 rows x BLOCK_N columns, 128B-swizzled), warps 2..9 restore H's tile
-// (64 rows x 128 columns) from global memory through registers into the layout that a swizzled TMA load would leave,
-// warp 1 issues tcgen05.mma on both as M/N-major operands, warps 10..13 take finished accumulators out of tensor memory.
-// H is the M operand, so that a thread of the epilogue holds one k and its warp stores 32 neighbouring k of a row of C.
+// Warp 0 fetches A's tiles by TMA (64 rows x 128-byte column blocks, 128B-swizzled), warps 2..9 restore H's tile (64 rows x
+// 128 columns) from global memory through registers into the layout that a swizzled TMA load would leave, warp 1 issues
+// tcgen05.mma on both as M/N-major operands, warps 10..13 take finished accumulators out of tensor memory.  H is the M
+// operand, so that a thread of the epilogue holds one k and its warp stores 32 neighbouring k of a row of C.
 //
-// A restored value has at most 8 significant bits (act8.cuh), so bf16 operands lose nothing of the codes.  Tensor memory
-// accumulates kChainBlocks k-blocks at a time; the epilogue adds such chains in fp32 in registers' rounding, which keeps the
-// error of long sums independent of the number of rows.
+// PAIR: two CTAs of a cluster compute 256 k x 256 n together (cta_group::2), each restoring its own 128 columns of H and
+// fetching half of A's columns: per k-block an SM takes in 16 KB of A and 8 KB of codes in place of 32 + 8 on a 128 x 256 tile of
+// its own, which is all that L2 delivers.
 //
-// Work is cut along the rows where there are fewer output tiles than SMs: every tile's rows are shared out to the same
-// number of CTAs in equal ranges, so that CTAs of different tiles walk the same rows at the same time and share them in L2;
-// partial results go to the workspace and a second kernel adds them in a fixed order.
+// A restored value has at most 8 significant bits (act8.cuh), so bf16 operands lose nothing of the codes.  The tensor cores
+// cut off what their accumulator does not hold rather than rounding it, an error that grows with the number of additions:
+// after kChainBlocks k-blocks the epilogue adds the accumulator to the part's sum with fp32 reductions in L2 (one thread,
+// one order: reproducible; sums below the normal range are flushed) and the next chain starts from zero.
+//
+// Work is cut along the rows where there are fewer output tiles than SMs.  Each tile's rows are shared out to `slices`
+// workers (a CTA or a pair) in equal ranges, so that workers of different tiles walk the same rows at the same time and share
+// them in L2; workers left over take the last rows of all tiles, in a row.  Partial tiles go to the workspace and a second
+// kernel adds them in a fixed order.
 #include <cstring>
 
 #include "act8.cuh"
@@ -24,71 +30,130 @@ namespace im {
 
 namespace {
 
-constexpr int kTileK = 128;                // columns of H per tile: the M of the instruction
+constexpr int kTileK = 128;                // columns of H per CTA: the M of the instruction, or half of it
 constexpr int kBlockRows = 64;             // rows of a k-block
 constexpr int kDecodeWarps = 8, kEpiWarps = 4;
 constexpr int kThreads = 32 * (2 + kDecodeWarps + kEpiWarps);
 constexpr int kMaxCtas = 160;              // (the workspace is sized for so many)
-constexpr int kChainBlocks = 32;           // k-blocks accumulated in tensor memory before they are added in fp32
+constexpr int kChainBlocks = 16;           // k-blocks accumulated in tensor memory before they are added in fp32
+constexpr int kAhead = 4;                  // k-blocks whose codes are on their way into a restoring thread's registers
 constexpr int kMaxCols = 65536;            // of either operand
 constexpr size_t kSmemLimit = 232448;
 
 struct Act8GemmParams {
     Act8View h;
     const float *gamma, *beta;             // or null: 1, 0
-    int relu;
     int R, Mo, No;                         // rows, columns of A, columns of H
     int tiles_k, tiles, kb;                // tiles along H's columns, all tiles, k-blocks of a tile
-    int slices;                            // CTAs sharing a tile
+    int workers;                           // CTAs or pairs
+    int slices, slice_kb;                  // workers per tile and their k-blocks (slices == 1 and no helpers: kb)
+    int helpers;                           // workers for the k-blocks behind slices * slice_kb of every tile
     float *C;
     long long ldc;
-    float *partial;                        // [tile * slices + slice][BLOCK_N][128]
+    float *partial;                        // [slot][tile rows (n)][tile columns (k)]; null: every part is a whole tile and goes to C
     uint32_t *status;
 };
 
-template <int BLOCK_N>
+template <int BLOCK_N, bool PAIR>
 struct Plan {
-    static constexpr int kABytes = kTileK * kBlockRows * 2, kBBytes = BLOCK_N * kBlockRows * 2, kStageBytes = kABytes + kBBytes;
+    static constexpr int kCols = PAIR ? 2 * kTileK : kTileK;                     // columns of H per tile
+    static constexpr int kACols = PAIR ? BLOCK_N / 2 : BLOCK_N;                  // columns of A that a CTA fetches
+    static constexpr int kHBytes = kTileK * kBlockRows * 2, kABytes = kACols * kBlockRows * 2, kStageBytes = kHBytes + kABytes;
     static constexpr int kStages = (int)((kSmemLimit - 2048) / kStageBytes) > 8 ? 8 : (int)((kSmemLimit - 2048) / kStageBytes);
     static constexpr int kTmemCols = 2 * BLOCK_N;
     static constexpr size_t kSmemBytes = 1024 + (size_t)kStages * kStageBytes + 512;
 };
 
-// The rows of a CTA's part of a tile, in k-blocks.
-__device__ __forceinline__ void part_blocks(const Act8GemmParams &P, int slice, int &k0, int &n)
+// The k-blocks [k0, k0 + n) of a tile, one after another for a worker; slot: where their sum goes.
+struct Part {
+    int tile, k0, n, slot;
+};
+// i-th part of worker w; false behind its last one.
+__device__ __forceinline__ bool part_at(const Act8GemmParams &P, int w, int i, Part &p)
 {
-    k0 = (int)((long long)slice * P.kb / P.slices);
-    n = (int)((long long)(slice + 1) * P.kb / P.slices) - k0;
+    const int mains = P.tiles * P.slices;
+    if (w < mains || !P.helpers) {
+        const int m = w + i * P.workers;
+        if (m >= mains || (P.helpers && i > 0)) return false;
+        const int slice = m / P.tiles;
+        p.tile = m - slice * P.tiles;
+        if (P.helpers) { p.k0 = slice * P.slice_kb; p.n = P.slice_kb; }
+        else {
+            p.k0 = (int)((long long)slice * P.kb / P.slices);
+            p.n = (int)((long long)(slice + 1) * P.kb / P.slices) - p.k0;
+        }
+        p.slot = p.tile * P.slices + slice;
+        return true;
+    }
+    const int h = w - mains, base = P.slices * P.slice_kb, rest = P.kb - base;
+    const long long units = (long long)P.tiles * rest, u1 = (long long)(h + 1) * units / P.helpers;
+    long long u = (long long)h * units / P.helpers;
+    u = i == 0 ? u : (u / rest + i) * rest;                          // (a tile after the first begins at its first block)
+    if (u >= u1) return false;
+    p.tile = (int)(u / rest);
+    const int in = (int)(u - (long long)p.tile * rest);
+    p.k0 = base + in;
+    p.n = (int)min((long long)(rest - in), u1 - u);
+    p.slot = mains + h + p.tile;
+    return true;
 }
 
-// Sixteen codes of one row to bf16, x16 columns of the swizzled tile: two 16-byte chunks.
-template <bool AFFINE>
-__device__ __forceinline__ void restore16(const uint4 &w, float s, int form, const float *ga, const float *be, bool relu, uint32_t (&out)[8])
+// Sixteen codes of one row to bf16.  MODE 0: code 2^e;  1: gamma code 2^e + beta;  2: the same under a ReLU.
+// kWide: as every scale allows; else for 2^e <= 2^100, where an int8 code's bits with the exponent of 2^23 are scaled and rid of
+// the 2^23 in one exact fused operation.
+template <int FORM, int MODE, bool kWide>
+__device__ __forceinline__ void restore16(const uint4 &w, float scale, const F2 *ga, const F2 *be, uint32_t (&out)[8])
 {
     const uint32_t u[4] = {w.x, w.y, w.z, w.w};
+    const F2 s = f2(scale), off = f2(-8388736.0f * scale);
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
-        float v[4];
-        act8_decode4(u[q], form, v);
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            v[j] *= s;
-            if (AFFINE) {
-                v[j] = __fmaf_rn(ga[4 * q + j], v[j], be[4 * q + j]);
-                if (relu) v[j] = v[j] < 0.0f ? 0.0f : v[j];               // (a NaN stays)
-            }
+        F2 v[2];
+        if (FORM == IM_ACT8_INT8 && !kWide) {
+            const uint32_t b = u[q] ^ 0x80808080u;
+            v[0] = fma2(f2(__uint_as_float(__byte_perm(b, 0x4b000000u, 0x7440)), __uint_as_float(__byte_perm(b, 0x4b000000u, 0x7441))), s, off);
+            v[1] = fma2(f2(__uint_as_float(__byte_perm(b, 0x4b000000u, 0x7442)), __uint_as_float(__byte_perm(b, 0x4b000000u, 0x7443))), s, off);
+        } else {
+            act8_decode4<FORM>(u[q], v[0], v[1]);
+            v[0] = mul2(v[0], s);
+            v[1] = mul2(v[1], s);
         }
-        __nv_bfloat162 h = __floats2bfloat162_rn(v[0], v[1]);
-        out[2 * q] = *reinterpret_cast<const uint32_t *>(&h);
-        h = __floats2bfloat162_rn(v[2], v[3]);
-        out[2 * q + 1] = *reinterpret_cast<const uint32_t *>(&h);
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            if (MODE) v[j] = fma2(ga[2 * q + j], v[j], be[2 * q + j]);
+            out[2 * q + j] = bf16x2<MODE == 2>(v[j]);
+        }
     }
 }
 
-template <int BLOCK_N, bool AFFINE>
-__global__ void __launch_bounds__(kThreads, 1) act8_tn_kernel(const __grid_constant__ CUtensorMap map_a, const Act8GemmParams P)
+// A wait on a barrier that CTAs of a cluster arrive on: their writes are visible after it.
+__device__ __forceinline__ bool mbar_try_wait_cluster(uint64_t *bar, uint32_t parity)
 {
-    using PL = Plan<BLOCK_N>;
+    uint32_t ok;
+    asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}"
+                 : "=r"(ok) : "r"(smem_u32(bar)), "r"(parity) : "memory");
+    return ok != 0;
+}
+template <bool PAIR>
+__device__ __forceinline__ bool wait_for(uint64_t *bar, uint32_t parity, volatile int *abort_flag)
+{
+    if (!mbar_wait(bar, parity, abort_flag)) return false;
+    if (PAIR) mbar_try_wait_cluster(bar, parity);           // (complete already: taken for its ordering)
+    return true;
+}
+
+// Arrives on the leader's barrier.  What a restoring warp publishes by it lies in its own CTA's shared memory and is read there by
+// that SM's tensor core, for which fence.proxy.async has ordered it before the arrive; a release at cluster scope on top costs
+// each k-block 900 cycles and more (measured; it waits for the thread's loads in flight), twice the rest of the work.
+__device__ __forceinline__ void mbar_arrive_leader(uint64_t *bar)
+{
+    asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(map_to_rank(smem_u32(bar), 0)) : "memory");
+}
+
+template <int BLOCK_N, bool PAIR, int FORM, int MODE>
+__device__ __forceinline__ void act8_tn_body(const CUtensorMap &map_a, const Act8GemmParams &P)
+{
+    using PL = Plan<BLOCK_N, PAIR>;
     extern __shared__ uint8_t smem_raw[];
     uint8_t *tiles = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
     uint64_t *full = reinterpret_cast<uint64_t *>(tiles + (size_t)PL::kStages * PL::kStageBytes);
@@ -96,153 +161,169 @@ __global__ void __launch_bounds__(kThreads, 1) act8_tn_kernel(const __grid_const
     uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(acc_empty + 2);
     volatile int *abort_flag = reinterpret_cast<volatile int *>(tmem_slot + 1);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const uint32_t rank = PAIR ? cluster_rank() : 0u;
+    const int worker = PAIR ? (int)blockIdx.x >> 1 : (int)blockIdx.x;
+    constexpr int kCtas = PAIR ? 2 : 1;
 
+    // full, acc_empty: of the pair's leader (rank 0), whose MMA thread waits on them; empty, acc_full: each CTA's own
     if (threadIdx.x == 0) {
-        for (int s = 0; s < PL::kStages; ++s) { mbar_init(&full[s], 1 + kDecodeWarps); mbar_init(&empty[s], 1); }
-        for (int a = 0; a < 2; ++a) { mbar_init(&acc_full[a], 1); mbar_init(&acc_empty[a], kEpiWarps); }
+        for (int s = 0; s < PL::kStages; ++s) { mbar_init(&full[s], 1 + kCtas * kDecodeWarps); mbar_init(&empty[s], 1); }
+        for (int a = 0; a < 2; ++a) { mbar_init(&acc_full[a], 1); mbar_init(&acc_empty[a], kCtas * kEpiWarps); }
         *abort_flag = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
-    if (warp == 1) tmem_alloc(tmem_slot, PL::kTmemCols);
+    if (warp == 1) {
+        if (PAIR) tmem_alloc_pair(tmem_slot, PL::kTmemCols);
+        else tmem_alloc(tmem_slot, PL::kTmemCols);
+    }
     tc_fence_before();
     __syncthreads();
+    if (PAIR) cluster_sync_all();                            // both CTAs' barriers exist before anyone signals them
     tc_fence_after();
     const uint32_t tmem_base = *tmem_slot;
+    if (PAIR && threadIdx.x == 0 && rank == 1) {
+        // the pair's MMAs address the accumulator at the same tensor-memory address in both CTAs
+        uint32_t leader_base;
+        asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(leader_base) : "r"(map_to_rank(smem_u32(tmem_slot), 0)) : "memory");
+        if (leader_base != tmem_base) *abort_flag = 1;
+    }
+    if (PAIR) __syncthreads();
 
-    const int parts = P.tiles * P.slices;
     int stage = 0, acc = 0;
     uint32_t phase = 0, acc_phase = 0;
+    bool ok = true;
+    Part part;
     if (warp == 0) {
         if (lane == 0 && !g_skip_loads)
-            for (int part = blockIdx.x; part < parts; part += gridDim.x) {
-                const int slice = part / P.tiles, tile = part - slice * P.tiles;
-                const int n0 = tile / P.tiles_k * BLOCK_N;
-                int k0, n;
-                part_blocks(P, slice, k0, n);
-                bool ok = true;
-                for (int i = 0; i < n && ok; ++i) {
+            for (int j = 0; ok && part_at(P, worker, j, part); ++j) {
+                const int n0 = part.tile / P.tiles_k * BLOCK_N + (int)rank * PL::kACols;
+                for (int i = 0; i < part.n; ++i) {
                     if (!(ok = mbar_wait(&empty[stage], phase ^ 1u, abort_flag))) break;
-                    uint8_t *sb = tiles + (size_t)stage * PL::kStageBytes + PL::kABytes;
-                    mbar_arrive_expect_tx(&full[stage], PL::kBBytes);
+                    uint8_t *sb = tiles + (size_t)stage * PL::kStageBytes + PL::kHBytes;
+                    const int row = (part.k0 + i) * kBlockRows;
+                    if (rank == 0) mbar_arrive_expect_tx(&full[stage], kCtas * PL::kABytes);
+                    const uint32_t bar = PAIR ? map_to_rank(smem_u32(&full[stage]), 0) : 0u;
 #pragma unroll
-                    for (int b = 0; b < BLOCK_N / 64; ++b) tma_load_2d(sb + b * 8192, &map_a, &full[stage], n0 + 64 * b, (k0 + i) * kBlockRows);
+                    for (int b = 0; b < PL::kACols / 64; ++b) {
+                        if (PAIR) tma_load_2d_pair(sb + b * 8192, &map_a, bar, n0 + 64 * b, row);
+                        else tma_load_2d(sb + b * 8192, &map_a, &full[stage], n0 + 64 * b, row);
+                    }
                     if (++stage == PL::kStages) { stage = 0; phase ^= 1u; }
                 }
-                if (!ok) break;
             }
     } else if (warp == 1) {
-        if (lane == 0) {
-            constexpr uint32_t idesc = instr_desc_bf16_mn(kTileK, BLOCK_N);
-            bool ok = true;
-            for (int part = blockIdx.x; part < parts && ok; part += gridDim.x) {
-                int k0, n;
-                part_blocks(P, part / P.tiles, k0, n);
-                for (int i = 0; i < n && ok; ++i) {
+        if (lane == 0 && rank == 0) {
+            constexpr uint32_t idesc = instr_desc_bf16_mn(kCtas * kTileK, BLOCK_N);
+            for (int j = 0; ok && part_at(P, worker, j, part); ++j) {
+                for (int i = 0; i < part.n; ++i) {
                     const int in_chain = i % kChainBlocks;
                     if (in_chain == 0) {
                         if (!(ok = mbar_wait(&acc_empty[acc], acc_phase ^ 1u, abort_flag))) break;
                         tc_fence_after();
                     }
-                    if (!(ok = mbar_wait(&full[stage], phase, abort_flag))) break;
+                    if (!(ok = wait_for<PAIR>(&full[stage], phase, abort_flag))) break;
                     tc_fence_after();
                     const uint32_t sa = smem_u32(tiles + (size_t)stage * PL::kStageBytes);
-                    const uint64_t da = smem_desc_mn_major_sw128(sa, 8192u), db = smem_desc_mn_major_sw128(sa + PL::kABytes, 8192u);
+                    const uint64_t dh = smem_desc_mn_major_sw128(sa, 8192u), da = smem_desc_mn_major_sw128(sa + PL::kHBytes, 8192u);
 #pragma unroll
-                    for (int k = 0; k < kBlockRows / 16; ++k)
-                        umma_bf16(tmem_base + (uint32_t)(acc * BLOCK_N), da + (uint64_t)(128 * k), db + (uint64_t)(128 * k), idesc, (in_chain | k) != 0 ? 1u : 0u);
-                    umma_commit(&empty[stage]);
+                    for (int k = 0; k < kBlockRows / 16; ++k) {
+                        const uint32_t d = tmem_base + (uint32_t)(acc * BLOCK_N), more = (in_chain | k) != 0 ? 1u : 0u;
+                        if (PAIR) umma_bf16_pair(d, dh + (uint64_t)(128 * k), da + (uint64_t)(128 * k), idesc, more);
+                        else umma_bf16(d, dh + (uint64_t)(128 * k), da + (uint64_t)(128 * k), idesc, more);
+                    }
+                    if (PAIR) umma_commit_pair(&empty[stage]);
+                    else umma_commit(&empty[stage]);
                     if (++stage == PL::kStages) { stage = 0; phase ^= 1u; }
-                    if (in_chain == kChainBlocks - 1 || i == n - 1) {
-                        umma_commit(&acc_full[acc]);
+                    if (in_chain == kChainBlocks - 1 || i == part.n - 1) {
+                        if (PAIR) umma_commit_pair(&acc_full[acc]);
+                        else umma_commit(&acc_full[acc]);
                         if (++acc == 2) { acc = 0; acc_phase ^= 1u; }
                     }
                 }
             }
         }
     } else if (warp < 2 + kDecodeWarps) {
-        // thread: 16 neighbouring columns (cq) of rows r and r + 32 of every k-block; eight threads cover a row of the tile
-        const int tid = (warp - 2) * 32 + lane, cq = tid & 7, r = tid >> 3;
-        const bool relu = P.relu != 0;
-        bool ok = true;
-        for (int part = blockIdx.x; part < parts && ok; part += gridDim.x) {
-            const int slice = part / P.tiles, tile = part - slice * P.tiles;
-            const int col = (tile % P.tiles_k) * kTileK + cq * 16;
-            int k0, n;
-            part_blocks(P, slice, k0, n);
-            float ga[16], be[16];
-            if (AFFINE) {
+        // thread: 16 neighbouring columns of rows r and r + 32 of every k-block.  Four lanes cover the 64 columns of a swizzled
+        // block, eight rows a warp: the eight lanes of a 16-byte store phase are two rows, whose swizzles differ in the lowest bit,
+        // and meet all banks.  The codes are asked for kAhead k-blocks before they are restored.
+        const int tid = (warp - 2) * 32 + lane, half = tid >> 7, cq = tid & 3, r = (tid >> 2) & 31;
+        const uint32_t at = (uint32_t)(half * 8192 + r * 128), c0 = (uint32_t)(((cq * 2) ^ (r & 7)) << 4), c1 = (uint32_t)(((cq * 2 + 1) ^ (r & 7)) << 4);
+        for (int j = 0; ok && part_at(P, worker, j, part); ++j) {
+            const int col = (part.tile % P.tiles_k) * PL::kCols + (int)rank * kTileK + half * 64 + cq * 16;
+            F2 ga[MODE ? 8 : 1], be[MODE ? 8 : 1];
+            if (MODE) {
 #pragma unroll
-                for (int j = 0; j < 16; ++j) {
-                    ga[j] = P.gamma && col + j < P.No ? __ldg(P.gamma + col + j) : 1.0f;
-                    be[j] = P.beta && col + j < P.No ? __ldg(P.beta + col + j) : 0.0f;
+                for (int c = 0; c < 8; ++c) {
+                    const auto at_col = [&](const float *p, int k, float other) { return p && k < P.No ? __ldg(p + k) : other; };
+                    ga[c] = f2(at_col(P.gamma, col + 2 * c, 1.0f), at_col(P.gamma, col + 2 * c + 1, 1.0f));
+                    be[c] = f2(at_col(P.beta, col + 2 * c, 0.0f), at_col(P.beta, col + 2 * c + 1, 0.0f));
                 }
             }
-            const bool in_cols = col < P.No;               // (rows are padded to 16 codes, so a chunk is readable as a whole)
-            uint4 w[2], w_next[2];
-            uint32_t byte[2], byte_next[2];
-            const auto fetch = [&](int i) {
-#pragma unroll
-                for (int q = 0; q < 2; ++q) {
-                    const long long row = (long long)(k0 + i) * kBlockRows + r + 32 * q;
-                    const bool in = in_cols && i < n && row < P.R;
-                    w_next[q] = in ? __ldg(reinterpret_cast<const uint4 *>(P.h.code + row * P.h.ld_code + col)) : make_uint4(0u, 0u, 0u, 0u);
-                    byte_next[q] = in ? __ldg(P.h.scale + row * P.h.ld_scale + (col >> 5)) : 256u;      // 256: nothing there, zeros
-                }
+            const long long row0 = (long long)part.k0 * kBlockRows + r;
+            const uint8_t *code = P.h.code + row0 * P.h.ld_code + col, *scale = P.h.scale + row0 * P.h.ld_scale + (col >> 5);
+            const long long code_half = 32 * P.h.ld_code, scale_half = 32 * P.h.ld_scale;
+            // rows of this thread in the part, from r on; none where the row has no such column (rows are padded to 16 codes, so a
+            // chunk that begins inside is readable as a whole)
+            const int rows_left = col < P.No ? (int)min((long long)part.n * kBlockRows - r, P.R - row0) : 0;
+            uint4 w[kAhead][2];
+            uint32_t byte[kAhead][2];
+            int ahead = rows_left;                            // rows left from the k-block that is fetched next
+            const auto fetch = [&](uint4 (&fw)[2], uint32_t (&fb)[2]) {
+                const bool in0 = ahead > 0, in1 = ahead > 32;
+                fw[0] = in0 ? __ldg(reinterpret_cast<const uint4 *>(code)) : make_uint4(0u, 0u, 0u, 0u);
+                fb[0] = in0 ? __ldg(scale) : 0u;
+                fw[1] = in1 ? __ldg(reinterpret_cast<const uint4 *>(code + code_half)) : make_uint4(0u, 0u, 0u, 0u);
+                fb[1] = in1 ? __ldg(scale + scale_half) : 0u;
+                code += 2 * code_half;
+                scale += 2 * scale_half;
+                ahead -= kBlockRows;
             };
-            fetch(0);
-            for (int i = 0; i < n; ++i) {
 #pragma unroll
-                for (int q = 0; q < 2; ++q) { w[q] = w_next[q]; byte[q] = byte_next[q]; }
-                fetch(i + 1);
-                if (!(ok = __all_sync(0xffffffffu, mbar_wait(&empty[stage], phase ^ 1u, abort_flag)))) break;
-                const uint32_t sa = smem_u32(tiles + (size_t)stage * PL::kStageBytes) + (uint32_t)((cq >> 2) * 8192);
+            for (int d = 0; d < kAhead; ++d) fetch(w[d], byte[d]);
+            for (int i0 = 0; ok && i0 < part.n; i0 += kAhead) {
 #pragma unroll
-                for (int q = 0; q < 2; ++q) {
-                    uint32_t o[8];
-                    restore16<AFFINE>(w[q], act8_scale(byte[q]), P.h.form, ga, be, relu, o);
-                    if (byte[q] == 256u) {
+                for (int d = 0; d < kAhead; ++d) {
+                    const int i = i0 + d;
+                    if (i >= part.n) break;
+                    if (!(ok = __all_sync(0xffffffffu, mbar_wait(&empty[stage], phase ^ 1u, abort_flag)))) break;
+                    const uint32_t dst = smem_u32(tiles + (size_t)stage * PL::kStageBytes) + at;
 #pragma unroll
-                        for (int j = 0; j < 8; ++j) o[j] = 0u;
+                    for (int q = 0; q < 2; ++q) {
+                        uint32_t o[8];
+                        if (FORM == IM_ACT8_INT8 && byte[d][q] > 227u) restore16<FORM, MODE, true>(w[d][q], act8_scale(byte[d][q]), ga, be, o);
+                        else restore16<FORM, MODE, false>(w[d][q], __uint_as_float(byte[d][q] << 23), ga, be, o);
+                        if (FORM != IM_ACT8_INT8 && byte[d][q] == 255u) {
+#pragma unroll
+                            for (int c = 0; c < 8; ++c) o[c] = 0x7fc07fc0u;
+                        }
+                        if (MODE && i * kBlockRows + 32 * q >= rows_left) {                 // behind the last row: zeros, not beta
+#pragma unroll
+                            for (int c = 0; c < 8; ++c) o[c] = 0u;
+                        }
+                        asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(dst + q * 4096 + c0), "r"(o[0]), "r"(o[1]), "r"(o[2]), "r"(o[3]) : "memory");
+                        asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(dst + q * 4096 + c1), "r"(o[4]), "r"(o[5]), "r"(o[6]), "r"(o[7]) : "memory");
                     }
-                    const int row = r + 32 * q;
-                    // lanes 4..7 of a row write the other 64-column half: in the opposite order, so that eight lanes meet all banks
-#pragma unroll
-                    for (int p = 0; p < 2; ++p) {
-                        const int c = p ^ (cq >> 2);
-                        const uint32_t dst = sa + (uint32_t)(row * 128) + (uint32_t)((((cq & 3) * 2 + c) ^ (row & 7)) << 4);
-                        asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(dst), "r"(c ? o[4] : o[0]), "r"(c ? o[5] : o[1]), "r"(c ? o[6] : o[2]),
-                                     "r"(c ? o[7] : o[3]) : "memory");
+                    fetch(w[d], byte[d]);
+                    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                    __syncwarp();
+                    if (lane == 0) {
+                        if (PAIR) mbar_arrive_leader(&full[stage]);
+                        else mbar_arrive(&full[stage]);
                     }
+                    if (++stage == PL::kStages) { stage = 0; phase ^= 1u; }
                 }
-                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-                __syncwarp();
-                if (lane == 0) mbar_arrive(&full[stage]);
-                if (++stage == PL::kStages) { stage = 0; phase ^= 1u; }
             }
         }
     } else {
         const int quad = warp & 3;                         // tensor-memory lanes 32 quad .. 32 quad + 31
-        bool ok = true;
-        for (int part = blockIdx.x; part < parts && ok; part += gridDim.x) {
-            const int slice = part / P.tiles, tile = part - slice * P.tiles;
-            const int n0 = tile / P.tiles_k * BLOCK_N, k = (tile % P.tiles_k) * kTileK + quad * 32 + lane;
-            int k0, n;
-            part_blocks(P, slice, k0, n);
+        for (int j = 0; ok && part_at(P, worker, j, part); ++j) {
+            const int n0 = part.tile / P.tiles_k * BLOCK_N, in_tile = (int)rank * kTileK + quad * 32 + lane;
+            const int k = (part.tile % P.tiles_k) * PL::kCols + in_tile;
             // where this thread's column goes, and how far apart its rows are
-            float *dst;
-            long long ld;
-            int rows = BLOCK_N;
-            bool in = true;
-            if (P.slices == 1) {
-                dst = P.C + (long long)n0 * P.ldc + k;
-                ld = P.ldc;
-                rows = min(BLOCK_N, P.Mo - n0);
-                in = k < P.No;
-            } else {
-                dst = P.partial + ((long long)tile * P.slices + slice) * (BLOCK_N * kTileK) + quad * 32 + lane;
-                ld = kTileK;
-            }
-            for (int i0 = 0; i0 < n; i0 += kChainBlocks) {
+            float *dst = P.partial ? P.partial + (long long)part.slot * (BLOCK_N * PL::kCols) + in_tile : P.C + (long long)n0 * P.ldc + k;
+            const long long ld = P.partial ? PL::kCols : P.ldc;
+            const int rows = k < P.No ? min(BLOCK_N, P.Mo - n0) : 0;
+            for (int i0 = 0; i0 < part.n; i0 += kChainBlocks) {
                 if (!(ok = __all_sync(0xffffffffu, mbar_wait(&acc_full[acc], acc_phase, abort_flag)))) break;
                 tc_fence_after();
                 const uint32_t t_row = tmem_base + ((uint32_t)(quad * 32) << 16) + (uint32_t)(acc * BLOCK_N);
@@ -251,21 +332,28 @@ __global__ void __launch_bounds__(kThreads, 1) act8_tn_kernel(const __grid_const
                     float v[32];
                     tmem_ld32_issue(t_row + (uint32_t)c0, v);
                     tmem_ld_wait();
+                    float *p = dst + (long long)c0 * ld;
+                    if (i0 == 0) {
 #pragma unroll
-                    for (int j = 0; j < 32; ++j) {
-                        if (!in || c0 + j >= rows) continue;
-                        float *p = dst + (long long)(c0 + j) * ld;
-                        *p = i0 == 0 ? v[j] : *p + v[j];
+                        for (int c = 0; c < 32; ++c)
+                            if (c0 + c < rows) p[(long long)c * ld] = v[c];
+                    } else {
+#pragma unroll
+                        for (int c = 0; c < 32; ++c)
+                            if (c0 + c < rows) asm volatile("red.relaxed.gpu.global.add.f32 [%0], %1;" ::"l"(p + (long long)c * ld), "f"(v[c]) : "memory");
                     }
                 }
                 tc_fence_before();
                 __syncwarp();
-                if (lane == 0) mbar_arrive(&acc_empty[acc]);
+                if (lane == 0) {
+                    if (PAIR) mbar_arrive_leader(&acc_empty[acc]);
+                    else mbar_arrive(&acc_empty[acc]);
+                }
                 if (++acc == 2) { acc = 0; acc_phase ^= 1u; }
             }
         }
     }
-    // everyone meets; the allocating warp frees tensor memory
+    // everyone meets (in a pair, so that shared memory and barriers outlive the peer's use of them); the allocating warp frees tensor memory
     if (*abort_flag && lane == 0) {
         // a wait ran out: copies and MMAs in flight get time to land (bounded)
         const unsigned long long t0 = global_ns();
@@ -274,26 +362,47 @@ __global__ void __launch_bounds__(kThreads, 1) act8_tn_kernel(const __grid_const
     tc_fence_before();
     __syncthreads();
     if (threadIdx.x == 0 && *abort_flag) atomicOr(P.status, IM_DEV_WAIT_TIMEOUT);
+    if (PAIR) cluster_sync_all();
     if (warp == 1) {
         tc_fence_after();
-        tmem_dealloc(tmem_base, PL::kTmemCols);
+        if (PAIR) tmem_dealloc_pair(tmem_base, PL::kTmemCols);
+        else tmem_dealloc(tmem_base, PL::kTmemCols);
     }
 }
-
-// C = the slices' partial tiles, added in order: a warp per 32 x 4 columns of one row.
-__global__ void __launch_bounds__(256) act8_tn_finish_kernel(const Act8GemmParams P, int block_n)
+template <int BLOCK_N, int FORM, int MODE>
+__global__ void __launch_bounds__(kThreads, 1) act8_tn_kernel(const __grid_constant__ CUtensorMap map_a, const Act8GemmParams P)
 {
-    const int lane = threadIdx.x & 31;
-    const int n = (int)blockIdx.y * 8 + (threadIdx.x >> 5), kt = blockIdx.x;
+    act8_tn_body<BLOCK_N, false, FORM, MODE>(map_a, P);
+}
+template <int FORM, int MODE>
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) act8_tn_pair_kernel(const __grid_constant__ CUtensorMap map_a, const Act8GemmParams P)
+{
+    act8_tn_body<256, true, FORM, MODE>(map_a, P);
+}
+
+// C = the partial tiles, added in a fixed order (slices, then helpers): a warp per 128 columns of one row.
+template <int BLOCK_N, bool PAIR>
+__global__ void __launch_bounds__(256) act8_tn_finish_kernel(const Act8GemmParams P)
+{
+    using PL = Plan<BLOCK_N, PAIR>;
+    constexpr long long kSlot = (long long)BLOCK_N * PL::kCols;
+    const int n = (int)blockIdx.y * 8 + (threadIdx.x >> 5), k = (int)blockIdx.x * 128 + (threadIdx.x & 31) * 4;
     if (n >= P.Mo) return;
-    const int tile = n / block_n * P.tiles_k + kt, row = n % block_n;
-    const float4 *src = reinterpret_cast<const float4 *>(P.partial + (long long)tile * P.slices * (block_n * kTileK) + row * kTileK) + lane;
-    float4 sum = src[0];
-    for (int s = 1; s < P.slices; ++s) {
-        const float4 v = src[(long long)s * (block_n * kTileK / 4)];
-        sum.x += v.x; sum.y += v.y; sum.z += v.z; sum.w += v.w;
+    const int tile = n / BLOCK_N * P.tiles_k + k / PL::kCols;
+    const float *src = P.partial + (long long)(n % BLOCK_N) * PL::kCols + k % PL::kCols;
+    const auto at = [&](long long slot) { return __ldg(reinterpret_cast<const float4 *>(src + slot * kSlot)); };
+    float4 sum = at((long long)tile * P.slices);
+    const auto add = [&](const float4 &v) { sum.x += v.x; sum.y += v.y; sum.z += v.z; sum.w += v.w; };
+    for (int s = 1; s < P.slices; ++s) add(at((long long)tile * P.slices + s));
+    if (P.helpers) {
+        const int rest = P.kb - P.slices * P.slice_kb;
+        const long long units = (long long)P.tiles * rest, u0 = (long long)tile * rest, u1 = u0 + rest;
+        for (int h = (int)(u0 * P.helpers / units); h < P.helpers; ++h) {              // helpers with units in [u0, u1)
+            const long long b = (long long)h * units / P.helpers, e = (long long)(h + 1) * units / P.helpers;
+            if (b >= u1) break;
+            if (e > u0 && e > b) add(at((long long)P.tiles * P.slices + h + tile));
+        }
     }
-    const int k = kt * kTileK + lane * 4;
     float *dst = P.C + (long long)n * P.ldc + k;
     if (k < P.No) dst[0] = sum.x;
     if (k + 1 < P.No) dst[1] = sum.y;
@@ -301,41 +410,63 @@ __global__ void __launch_bounds__(256) act8_tn_finish_kernel(const Act8GemmParam
     if (k + 3 < P.No) dst[3] = sum.w;
 }
 
-int block_n_for(int Mo) { return Mo <= 64 ? 64 : Mo <= 128 ? 128 : 256; }
-
+// Tile shape and split.  Narrow A: one CTA per tile, 64 or 128 columns; else pairs with 256, unless H is too narrow for both CTAs.
 struct Split {
-    int block_n, tiles_k, tiles, kb, slices;
+    int block_n;
+    bool pair;
+    int tiles_k, tiles, kb, workers, slices, slice_kb, helpers;
+    size_t slot_bytes() const { return (size_t)block_n * (pair ? 2 : 1) * kTileK * sizeof(float); }
+    bool whole() const { return slices == 1 && helpers == 0; }
 };
+constexpr int kLeastBlocks = 4;            // k-blocks of a part, at least
+constexpr int kHelpFrom = 32;              // k-blocks per worker from which helpers pay for their extra parts
 Split split_for(int R, int Mo, int No, int ctas)
 {
     Split s;
-    s.block_n = block_n_for(Mo);
-    s.tiles_k = (No + kTileK - 1) / kTileK;
+    s.pair = Mo > 128 && No > kTileK;
+    s.block_n = s.pair ? 256 : Mo <= 64 ? 64 : 128;
+    s.workers = s.pair ? ctas / 2 : ctas;
+    const int cols = s.pair ? 2 * kTileK : kTileK;
+    s.tiles_k = (No + cols - 1) / cols;
     s.tiles = s.tiles_k * ((Mo + s.block_n - 1) / s.block_n);
     s.kb = (R + kBlockRows - 1) / kBlockRows;
-    s.slices = ctas / s.tiles;
-    const int most = (s.kb + 3) / 4;                        // four k-blocks at least
+    const int most = s.kb / kLeastBlocks;
+    s.slices = s.workers / s.tiles;
     s.slices = s.slices < most ? s.slices : most;
     s.slices = s.slices < 1 ? 1 : s.slices;
+    s.slice_kb = s.kb;
+    s.helpers = 0;
+    const int left = s.workers - s.tiles * s.slices;
+    const long long share = (long long)s.kb * s.tiles / s.workers;                 // k-blocks per worker, if all are busy
+    if (left > 0 && share >= kHelpFrom && s.workers / s.tiles == s.slices) {
+        s.helpers = left;
+        s.slice_kb = (int)share;
+    }
     return s;
 }
-size_t partial_bytes(const Split &s) { return s.slices == 1 ? 0 : (size_t)s.tiles * s.slices * s.block_n * kTileK * sizeof(float); }
 
-template <int BLOCK_N, bool AFFINE>
-cudaError_t launch_product(const CUtensorMap &map, const Act8GemmParams &p, int grid, cudaStream_t st)
+template <int FORM, int MODE>
+cudaError_t launch_product(const Split &s, const CUtensorMap &map, const Act8GemmParams &p, int grid, cudaStream_t st)
 {
     static DeviceOnce once;
-    const cudaError_t e = once.run([] {
-        return cudaFuncSetAttribute(act8_tn_kernel<BLOCK_N, AFFINE>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)Plan<BLOCK_N>::kSmemBytes);
+    const auto k64 = act8_tn_kernel<64, FORM, MODE>, k128 = act8_tn_kernel<128, FORM, MODE>, kpair = act8_tn_pair_kernel<FORM, MODE>;
+    const cudaError_t e = once.run([&] {
+        cudaError_t r = cudaFuncSetAttribute(k64, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)Plan<64, false>::kSmemBytes);
+        if (r == cudaSuccess) r = cudaFuncSetAttribute(k128, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)Plan<128, false>::kSmemBytes);
+        if (r == cudaSuccess) r = cudaFuncSetAttribute(kpair, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)Plan<256, true>::kSmemBytes);
+        return r;
     });
     if (e != cudaSuccess) return e;
-    act8_tn_kernel<BLOCK_N, AFFINE><<<grid, kThreads, Plan<BLOCK_N>::kSmemBytes, st>>>(map, p);
+    if (s.pair) kpair<<<grid, kThreads, Plan<256, true>::kSmemBytes, st>>>(map, p);
+    else if (s.block_n == 64) k64<<<grid, kThreads, Plan<64, false>::kSmemBytes, st>>>(map, p);
+    else k128<<<grid, kThreads, Plan<128, false>::kSmemBytes, st>>>(map, p);
     return cudaGetLastError();
 }
-template <int BLOCK_N>
-cudaError_t launch_product(const CUtensorMap &map, const Act8GemmParams &p, bool affine, int grid, cudaStream_t st)
+template <int FORM>
+cudaError_t launch_product(const Split &s, const CUtensorMap &map, const Act8GemmParams &p, int mode, int grid, cudaStream_t st)
 {
-    return affine ? launch_product<BLOCK_N, true>(map, p, grid, st) : launch_product<BLOCK_N, false>(map, p, grid, st);
+    return mode == 0 ? launch_product<FORM, 0>(s, map, p, grid, st)
+         : mode == 1 ? launch_product<FORM, 1>(s, map, p, grid, st) : launch_product<FORM, 2>(s, map, p, grid, st);
 }
 
 }  // namespace
@@ -355,7 +486,10 @@ size_t im_gemm_act8_tn_workspace_bytes(int32_t R, int32_t Mo, int32_t No)
 {
     using namespace im;
     if (R < 1 || Mo < 1 || No < 1) return 0;
-    return partial_bytes(split_for(R, Mo, No, kMaxCtas));
+    // for as many SMs as there may be: a slot per worker, and one more per tile for helpers whose range crosses tiles
+    const Split s = split_for(R, Mo, No, kMaxCtas);
+    if (s.tiles >= s.workers || s.kb < 2 * kLeastBlocks) return 0;
+    return (size_t)(s.workers + s.tiles) * s.slot_bytes();
 }
 
 im_status im_gemm_act8_tn(const uint16_t *A, int64_t lda, const im_act8 *H, float *C, int64_t ldc, int32_t R, int32_t Mo, int32_t No, const float *gamma,
@@ -375,17 +509,21 @@ im_status im_gemm_act8_tn(const uint16_t *A, int64_t lda, const im_act8 *H, floa
     const Split s = split_for(R, Mo, No, n_sm);
     Act8GemmParams p;
     std::memset(&p, 0, sizeof(p));
-    p.h = act8_view(H); p.gamma = gamma; p.beta = beta; p.relu = relu != 0;
-    p.R = R; p.Mo = Mo; p.No = No; p.tiles_k = s.tiles_k; p.tiles = s.tiles; p.kb = s.kb; p.slices = s.slices;
-    p.C = C; p.ldc = ldc; p.partial = static_cast<float *>(workspace); p.status = status;
-    const bool affine = gamma || beta || relu;
-    const int parts = s.tiles * s.slices, grid = parts < n_sm ? parts : n_sm;
+    p.h = act8_view(H); p.gamma = gamma; p.beta = beta;
+    p.R = R; p.Mo = Mo; p.No = No; p.tiles_k = s.tiles_k; p.tiles = s.tiles; p.kb = s.kb;
+    p.workers = s.workers; p.slices = s.slices; p.slice_kb = s.slice_kb; p.helpers = s.helpers;
+    p.C = C; p.ldc = ldc; p.partial = s.whole() ? nullptr : static_cast<float *>(workspace); p.status = status;
+    const int mode = relu ? 2 : gamma || beta ? 1 : 0;
+    const int busy = s.helpers || s.tiles * s.slices >= s.workers ? s.workers : s.tiles * s.slices;
+    const int grid = s.pair ? 2 * busy : busy;
     cudaStream_t st = (cudaStream_t)cuda_stream;
-    cudaError_t e = s.block_n == 64 ? launch_product<64>(map, p, affine, grid, st)
-                  : s.block_n == 128 ? launch_product<128>(map, p, affine, grid, st) : launch_product<256>(map, p, affine, grid, st);
+    cudaError_t e = H->form == IM_ACT8_INT8 ? launch_product<IM_ACT8_INT8>(s, map, p, mode, grid, st) : launch_product<IM_ACT8_E4M3>(s, map, p, mode, grid, st);
     g_launches.fetch_add(1, std::memory_order_relaxed);
-    if (e == cudaSuccess && s.slices > 1) {
-        act8_tn_finish_kernel<<<dim3((unsigned)s.tiles_k, (unsigned)((Mo + 7) / 8)), 256, 0, st>>>(p, s.block_n);
+    if (e == cudaSuccess && p.partial) {
+        const dim3 fin((unsigned)((No + 127) / 128), (unsigned)((Mo + 7) / 8));
+        if (s.pair) act8_tn_finish_kernel<256, true><<<fin, 256, 0, st>>>(p);
+        else if (s.block_n == 64) act8_tn_finish_kernel<64, false><<<fin, 256, 0, st>>>(p);
+        else act8_tn_finish_kernel<128, false><<<fin, 256, 0, st>>>(p);
         g_launches.fetch_add(1, std::memory_order_relaxed);
         e = cudaGetLastError();
     }

@@ -81,7 +81,7 @@ def test_workspace_sizes(lib):
     assert lib.im_layer_norm_workspace_bytes(10 ** 6, 1024) == 592 * 2 * 1024 * 4
     assert lib.im_gemm_act8_tn_workspace_bytes(64, 64, 64) == 0                      # one k-block: one part per tile
     sizes = [lib.im_gemm_act8_tn_workspace_bytes(r, 512, 1024) for r in (64, 1000, 10000, 100000, 10 ** 6)]
-    assert sizes == sorted(sizes) and sizes[-1] == sizes[-2] <= 160 * 128 * 256 * 4
+    assert sizes == sorted(sizes) and sizes[-1] == sizes[-2] == (80 + 8) * 256 * 256 * 4      # 80 pairs, 8 tiles
     assert lib.im_gemm_act8_tn_workspace_bytes(-1, 1, 1) == 0
 
 
