@@ -586,7 +586,7 @@ im_status im_colsum_f32(const float *x, int64_t ld, int64_t rows, int32_t cols, 
  * im_gemm_act8_tn: the weight gradient of the layer above,  C[n][k] = sum_r A[r][n] H[r][k],  n < Mo, k < No, on the
  *   tensor cores with H restored on the way in: the values im_act8_unpack would give as bf16.  A bf16 [R][lda] (lda a multiple of 8,
  *   16-byte aligned), C float [Mo][ldc].  H->code 16-byte aligned with ld_code a multiple of 16 and whole rows readable (R ld_code
- *   bytes).  R, Mo and No need not be multiples of anything; Mo, No <= 65536 (IM_ERR_UNSUPPORTED beyond).  workspace: as
+ *   bytes).  R, Mo and No need not be multiples of anything; Mo, No <= 65536, R < 2^31 - 2^16, H's strides < 2^31 (IM_ERR_UNSUPPORTED beyond).  workspace: as
  *   above, im_gemm_act8_tn_workspace_bytes(R, Mo, No) bytes (which may be 0: then NULL will do).  status DEVICE uint32 [1] receives
  *   IM_DEV_WAIT_TIMEOUT if a bounded wait inside the kernel runs out. */
 #define IM_DTYPE_F32  0

@@ -1,9 +1,9 @@
 // Weight gradient from an 8-bit checkpoint: C[n][k] = sum over rows r of A[r][n] H[r][k], A bf16 (the gradient at a layer's
 // pre-activation), H restored from im_act8: code 2^e, or bf16(act(gamma code 2^e + beta)).  fp32 accumulation and output.
 //
-// Warp 0 fetches A's tiles by TMA (64 rows x 128-byte column blocks, 128B-swizzled), warps 2..9 restore H's tile (64 rows x
+// Warp 0 fetches A's tiles by TMA (64 rows x 128-byte column blocks, 128B-swizzled), warps 2..17 restore H's tile (64 rows x
 // 128 columns) from global memory through registers into the layout that a swizzled TMA load would leave, warp 1 issues
-// tcgen05.mma on both as M/N-major operands, warps 10..13 take finished accumulators out of tensor memory.  H is the M
+// tcgen05.mma on both as M/N-major operands, warps 18..21 take finished accumulators out of tensor memory.  H is the M
 // operand, so that a thread of the epilogue holds one k and its warp stores 32 neighbouring k of a row of C.
 //
 // PAIR: two CTAs of a cluster compute 256 k x 256 n together (cta_group::2), each restoring its own 128 columns of H and
@@ -12,8 +12,8 @@
 //
 // A restored value has at most 8 significant bits (act8.cuh), so bf16 operands lose nothing of the codes.  The tensor cores
 // cut off what their accumulator does not hold rather than rounding it, an error that grows with the number of additions:
-// after kChainBlocks k-blocks the epilogue adds the accumulator to the part's sum with fp32 reductions in L2 (one thread,
-// one order: reproducible; sums below the normal range are flushed) and the next chain starts from zero.
+// after kChainBlocks k-blocks the epilogue adds the accumulator to the part's sum, which lies in tensor memory too, and the next chain
+// starts from zero.
 //
 // Work is cut along the rows where there are fewer output tiles than SMs.  Each tile's rows are shared out to `slices`
 // workers (a CTA or a pair) in equal ranges, so that workers of different tiles walk the same rows at the same time and share
@@ -32,12 +32,13 @@ namespace {
 
 constexpr int kTileK = 128;                // columns of H per CTA: the M of the instruction, or half of it
 constexpr int kBlockRows = 64;             // rows of a k-block
-constexpr int kDecodeWarps = 8, kEpiWarps = 4;
+constexpr int kDecodeWarps = 16, kEpiWarps = 4;
 constexpr int kThreads = 32 * (2 + kDecodeWarps + kEpiWarps);
 constexpr int kMaxCtas = 160;              // (the workspace is sized for so many)
 constexpr int kChainBlocks = 16;           // k-blocks accumulated in tensor memory before they are added in fp32
-constexpr int kAhead = 4;                  // k-blocks whose codes are on their way into a restoring thread's registers
+constexpr int kBatch = 2;                  // k-blocks whose codes a restoring thread asks for together, a batch ahead
 constexpr int kMaxCols = 65536;            // of either operand
+constexpr int kMaxRows = 0x7fff0000, kMaxStride = 0x7fffffff;               // row numbers (a k-block or two beyond the last) and strides of H in 32 bits
 constexpr size_t kSmemLimit = 232448;
 
 struct Act8GemmParams {
@@ -60,7 +61,8 @@ struct Plan {
     static constexpr int kACols = PAIR ? BLOCK_N / 2 : BLOCK_N;                  // columns of A that a CTA fetches
     static constexpr int kHBytes = kTileK * kBlockRows * 2, kABytes = kACols * kBlockRows * 2, kStageBytes = kHBytes + kABytes;
     static constexpr int kStages = (int)((kSmemLimit - 2048) / kStageBytes) > 8 ? 8 : (int)((kSmemLimit - 2048) / kStageBytes);
-    static constexpr int kTmemCols = 2 * BLOCK_N;
+    static constexpr int kAccs = PAIR ? 1 : 2;                                   // accumulators; behind them the sum of finished chains
+    static constexpr int kTmemCols = BLOCK_N == 64 ? 256 : 512;                  // at least (kAccs + 1) BLOCK_N, a power of two
     static constexpr size_t kSmemBytes = 1024 + (size_t)kStages * kStageBytes + 512;
 };
 
@@ -98,57 +100,70 @@ __device__ __forceinline__ bool part_at(const Act8GemmParams &P, int w, int i, P
     return true;
 }
 
-// Sixteen codes of one row to bf16.  MODE 0: code 2^e;  1: gamma code 2^e + beta;  2: the same under a ReLU.
-// kWide: as every scale allows; else for 2^e <= 2^100, where an int8 code's bits with the exponent of 2^23 are scaled and rid of
-// the 2^23 in one exact fused operation.
-template <int FORM, int MODE, bool kWide>
-__device__ __forceinline__ void restore16(const uint4 &w, float scale, const F2 *ga, const F2 *be, uint32_t (&out)[8])
+// Eight codes of one row to bf16.  MODE 0: code 2^e;  1: gamma code 2^e + beta;  2: the same under a ReLU.
+template <int FORM, int MODE>
+__device__ __forceinline__ void restore8(const uint2 &w, float scale, const F2 *ga, const F2 *be, uint32_t (&out)[4])
 {
-    const uint32_t u[4] = {w.x, w.y, w.z, w.w};
-    const F2 s = f2(scale), off = f2(-8388736.0f * scale);
+    const F2 s = f2(scale);
+    F2 v[4];
+    act8_decode4<FORM>(w.x, v[0], v[1]);
+    act8_decode4<FORM>(w.y, v[2], v[3]);
 #pragma unroll
-    for (int q = 0; q < 4; ++q) {
-        F2 v[2];
-        if (FORM == IM_ACT8_INT8 && !kWide) {
-            const uint32_t b = u[q] ^ 0x80808080u;
-            v[0] = fma2(f2(__uint_as_float(__byte_perm(b, 0x4b000000u, 0x7440)), __uint_as_float(__byte_perm(b, 0x4b000000u, 0x7441))), s, off);
-            v[1] = fma2(f2(__uint_as_float(__byte_perm(b, 0x4b000000u, 0x7442)), __uint_as_float(__byte_perm(b, 0x4b000000u, 0x7443))), s, off);
-        } else {
-            act8_decode4<FORM>(u[q], v[0], v[1]);
-            v[0] = mul2(v[0], s);
-            v[1] = mul2(v[1], s);
-        }
-#pragma unroll
-        for (int j = 0; j < 2; ++j) {
-            if (MODE) v[j] = fma2(ga[2 * q + j], v[j], be[2 * q + j]);
-            out[2 * q + j] = bf16x2<MODE == 2>(v[j]);
-        }
+    for (int j = 0; j < 4; ++j) {
+        v[j] = mul2(v[j], s);
+        if (MODE) v[j] = fma2(ga[j], v[j], be[j]);
+        out[j] = bf16x2<MODE == 2>(v[j]);
     }
 }
 
-// A wait on a barrier that CTAs of a cluster arrive on: their writes are visible after it.
-__device__ __forceinline__ bool mbar_try_wait_cluster(uint64_t *bar, uint32_t parity)
+// Loads that keep their place: the compiler would move them down to their first use.
+__device__ __forceinline__ uint2 load_codes(const uint8_t *p)
+{
+    uint2 w;
+    asm volatile("ld.global.nc.L1::no_allocate.v2.b32 {%0, %1}, [%2];" : "=r"(w.x), "=r"(w.y) : "l"(p));
+    return w;
+}
+__device__ __forceinline__ uint32_t load_byte(const uint8_t *p)
+{
+    uint32_t b;
+    asm volatile("ld.global.nc.u8 %0, [%1];" : "=r"(b) : "l"(p));
+    return b;
+}
+__device__ __forceinline__ bool mbar_test(uint64_t *bar, uint32_t parity)
 {
     uint32_t ok;
-    asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}"
+    asm volatile("{\n\t.reg .pred p;\n\tmbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}"
                  : "=r"(ok) : "r"(smem_u32(bar)), "r"(parity) : "memory");
     return ok != 0;
 }
-template <bool PAIR>
-__device__ __forceinline__ bool wait_for(uint64_t *bar, uint32_t parity, volatile int *abort_flag)
-{
-    if (!mbar_wait(bar, parity, abort_flag)) return false;
-    if (PAIR) mbar_try_wait_cluster(bar, parity);           // (complete already: taken for its ordering)
-    return true;
-}
 
-// Arrives on the leader's barrier.  What a restoring warp publishes by it lies in its own CTA's shared memory and is read there by
-// that SM's tensor core, for which fence.proxy.async has ordered it before the arrive; a release at cluster scope on top costs
-// each k-block 900 cycles and more (measured; it waits for the thread's loads in flight), twice the rest of the work.
-__device__ __forceinline__ void mbar_arrive_leader(uint64_t *bar)
+__device__ __forceinline__ void tmem_st32(uint32_t taddr, const float *v)
 {
-    asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(map_to_rank(smem_u32(bar), 0)) : "memory");
+    const uint32_t *r = reinterpret_cast<const uint32_t *>(v);
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x32.b32 [%32], "
+                 "{%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,"
+                 "%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31};"
+                 ::"r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]),
+                   "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]),
+                   "r"(r[16]), "r"(r[17]), "r"(r[18]), "r"(r[19]), "r"(r[20]), "r"(r[21]), "r"(r[22]), "r"(r[23]),
+                   "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]), "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31]), "r"(taddr) : "memory");
 }
+// One lane of a converged warp, the same every time.
+__device__ __forceinline__ bool elect_one()
+{
+    uint32_t p;
+    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(p));
+    return p != 0;
+}
+// Arrives on a barrier of the pair's leader (map_to_rank).  What a restoring warp publishes by it lies in its own CTA's shared
+// memory and is read there by that SM's tensor core, for which fence.proxy.async has ordered it before the arrive; a release at
+// cluster scope on top costs each k-block 900 cycles and more (measured; it waits for the thread's loads in flight), twice the
+// rest of the work.
+__device__ __forceinline__ void mbar_arrive_remote(uint32_t cluster_addr)
+{
+    asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(cluster_addr) : "memory");
+}
+__device__ __forceinline__ void mbar_arrive_addr(uint32_t addr) { asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(addr) : "memory"); }
 
 template <int BLOCK_N, bool PAIR, int FORM, int MODE>
 __device__ __forceinline__ void act8_tn_body(const CUtensorMap &map_a, const Act8GemmParams &P)
@@ -193,125 +208,147 @@ __device__ __forceinline__ void act8_tn_body(const CUtensorMap &map_a, const Act
     uint32_t phase = 0, acc_phase = 0;
     bool ok = true;
     Part part;
+    // The loops of the producer and of the MMA issuer are run by their whole warps, which keeps addresses and descriptors in
+    // uniform registers; an elected lane issues.
     if (warp == 0) {
-        if (lane == 0 && !g_skip_loads)
+        const bool one = elect_one();
+        const uint32_t full0 = PAIR ? map_to_rank(smem_u32(full), 0) : 0u;
+        if (!g_skip_loads)
             for (int j = 0; ok && part_at(P, worker, j, part); ++j) {
                 const int n0 = part.tile / P.tiles_k * BLOCK_N + (int)rank * PL::kACols;
-                for (int i = 0; i < part.n; ++i) {
-                    if (!(ok = mbar_wait(&empty[stage], phase ^ 1u, abort_flag))) break;
+                int row = part.k0 * kBlockRows;
+                for (int i = 0; i < part.n; ++i, row += kBlockRows) {
+                    if (!(ok = __all_sync(0xffffffffu, mbar_wait(&empty[stage], phase ^ 1u, abort_flag)))) break;
                     uint8_t *sb = tiles + (size_t)stage * PL::kStageBytes + PL::kHBytes;
-                    const int row = (part.k0 + i) * kBlockRows;
-                    if (rank == 0) mbar_arrive_expect_tx(&full[stage], kCtas * PL::kABytes);
-                    const uint32_t bar = PAIR ? map_to_rank(smem_u32(&full[stage]), 0) : 0u;
+                    if (one) {
+                        if (rank == 0) mbar_arrive_expect_tx(&full[stage], kCtas * PL::kABytes);
 #pragma unroll
-                    for (int b = 0; b < PL::kACols / 64; ++b) {
-                        if (PAIR) tma_load_2d_pair(sb + b * 8192, &map_a, bar, n0 + 64 * b, row);
-                        else tma_load_2d(sb + b * 8192, &map_a, &full[stage], n0 + 64 * b, row);
+                        for (int b = 0; b < PL::kACols / 64; ++b) {
+                            if (PAIR) tma_load_2d_pair(sb + b * 8192, &map_a, full0 + (uint32_t)(stage * 8), n0 + 64 * b, row);
+                            else tma_load_2d(sb + b * 8192, &map_a, &full[stage], n0 + 64 * b, row);
+                        }
                     }
+                    __syncwarp();
                     if (++stage == PL::kStages) { stage = 0; phase ^= 1u; }
                 }
             }
     } else if (warp == 1) {
-        if (lane == 0 && rank == 0) {
+        if (rank == 0) {
             constexpr uint32_t idesc = instr_desc_bf16_mn(kCtas * kTileK, BLOCK_N);
+            const bool one = elect_one();
+            const uint64_t dh0 = smem_desc_mn_major_sw128(smem_u32(tiles), 8192u), da0 = smem_desc_mn_major_sw128(smem_u32(tiles) + PL::kHBytes, 8192u);
             for (int j = 0; ok && part_at(P, worker, j, part); ++j) {
+                int in_chain = 0;
                 for (int i = 0; i < part.n; ++i) {
-                    const int in_chain = i % kChainBlocks;
                     if (in_chain == 0) {
-                        if (!(ok = mbar_wait(&acc_empty[acc], acc_phase ^ 1u, abort_flag))) break;
-                        tc_fence_after();
+                        if (!(ok = __all_sync(0xffffffffu, mbar_wait(&acc_empty[acc], acc_phase ^ 1u, abort_flag)))) break;
                     }
-                    if (!(ok = wait_for<PAIR>(&full[stage], phase, abort_flag))) break;
+                    if (!(ok = __all_sync(0xffffffffu, mbar_wait(&full[stage], phase, abort_flag)))) break;
                     tc_fence_after();
-                    const uint32_t sa = smem_u32(tiles + (size_t)stage * PL::kStageBytes);
-                    const uint64_t dh = smem_desc_mn_major_sw128(sa, 8192u), da = smem_desc_mn_major_sw128(sa + PL::kHBytes, 8192u);
+                    const uint32_t d = tmem_base + (uint32_t)(acc * BLOCK_N);
+                    const uint64_t step = (uint64_t)(uint32_t)(stage * (PL::kStageBytes >> 4)), dh = dh0 + step, da = da0 + step;
+                    const bool last = in_chain == kChainBlocks - 1 || i == part.n - 1;
+                    if (one) {
 #pragma unroll
-                    for (int k = 0; k < kBlockRows / 16; ++k) {
-                        const uint32_t d = tmem_base + (uint32_t)(acc * BLOCK_N), more = (in_chain | k) != 0 ? 1u : 0u;
-                        if (PAIR) umma_bf16_pair(d, dh + (uint64_t)(128 * k), da + (uint64_t)(128 * k), idesc, more);
-                        else umma_bf16(d, dh + (uint64_t)(128 * k), da + (uint64_t)(128 * k), idesc, more);
+                        for (int k = 0; k < kBlockRows / 16; ++k) {
+                            const uint32_t more = (in_chain | k) != 0 ? 1u : 0u;
+                            if (PAIR) umma_bf16_pair(d, dh + (uint64_t)(128 * k), da + (uint64_t)(128 * k), idesc, more);
+                            else umma_bf16(d, dh + (uint64_t)(128 * k), da + (uint64_t)(128 * k), idesc, more);
+                        }
+                        if (PAIR) umma_commit_pair(&empty[stage]);
+                        else umma_commit(&empty[stage]);
+                        if (last) {
+                            if (PAIR) umma_commit_pair(&acc_full[acc]);
+                            else umma_commit(&acc_full[acc]);
+                        }
                     }
-                    if (PAIR) umma_commit_pair(&empty[stage]);
-                    else umma_commit(&empty[stage]);
+                    __syncwarp();
                     if (++stage == PL::kStages) { stage = 0; phase ^= 1u; }
-                    if (in_chain == kChainBlocks - 1 || i == part.n - 1) {
-                        if (PAIR) umma_commit_pair(&acc_full[acc]);
-                        else umma_commit(&acc_full[acc]);
-                        if (++acc == 2) { acc = 0; acc_phase ^= 1u; }
+                    ++in_chain;
+                    if (last) {
+                        in_chain = 0;
+                        if (++acc == PL::kAccs) { acc = 0; acc_phase ^= 1u; }
                     }
                 }
             }
         }
     } else if (warp < 2 + kDecodeWarps) {
-        // thread: 16 neighbouring columns of rows r and r + 32 of every k-block.  Four lanes cover the 64 columns of a swizzled
-        // block, eight rows a warp: the eight lanes of a 16-byte store phase are two rows, whose swizzles differ in the lowest bit,
-        // and meet all banks.  The codes are asked for kAhead k-blocks before they are restored.
-        const int tid = (warp - 2) * 32 + lane, half = tid >> 7, cq = tid & 3, r = (tid >> 2) & 31;
-        const uint32_t at = (uint32_t)(half * 8192 + r * 128), c0 = (uint32_t)(((cq * 2) ^ (r & 7)) << 4), c1 = (uint32_t)(((cq * 2 + 1) ^ (r & 7)) << 4);
+        // thread: 8 neighbouring columns of rows r and r + 32 of every k-block.  Eight lanes cover the 64 columns of a swizzled block
+        // row, so that a 16-byte store phase meets all banks; with 8 columns gamma and beta take 16 registers, which leaves room
+        // for the 16 warps that hide the latencies of loads, barriers and conversions.  Codes are asked for in batches, a batch
+        // ahead: one wait for all loads of a batch.
+        const int tid = (warp - 2) * 32 + lane, half = tid >> 8, cq = tid & 7, r = (tid >> 3) & 31;
+        const uint32_t tile0 = smem_u32(tiles) + (uint32_t)(half * 8192 + r * 128) + (uint32_t)((cq ^ (r & 7)) << 4);
+        const uint32_t full0 = PAIR ? map_to_rank(smem_u32(full), 0) : smem_u32(full);
+        bool ready = mbar_test(&empty[0], 1u);
         for (int j = 0; ok && part_at(P, worker, j, part); ++j) {
-            const int col = (part.tile % P.tiles_k) * PL::kCols + (int)rank * kTileK + half * 64 + cq * 16;
-            F2 ga[MODE ? 8 : 1], be[MODE ? 8 : 1];
+            const int col = (part.tile % P.tiles_k) * PL::kCols + (int)rank * kTileK + half * 64 + cq * 8;
+            F2 ga[MODE ? 4 : 1], be[MODE ? 4 : 1];
             if (MODE) {
 #pragma unroll
-                for (int c = 0; c < 8; ++c) {
+                for (int c = 0; c < 4; ++c) {
                     const auto at_col = [&](const float *p, int k, float other) { return p && k < P.No ? __ldg(p + k) : other; };
                     ga[c] = f2(at_col(P.gamma, col + 2 * c, 1.0f), at_col(P.gamma, col + 2 * c + 1, 1.0f));
                     be[c] = f2(at_col(P.beta, col + 2 * c, 0.0f), at_col(P.beta, col + 2 * c + 1, 0.0f));
                 }
             }
-            const long long row0 = (long long)part.k0 * kBlockRows + r;
-            const uint8_t *code = P.h.code + row0 * P.h.ld_code + col, *scale = P.h.scale + row0 * P.h.ld_scale + (col >> 5);
-            const long long code_half = 32 * P.h.ld_code, scale_half = 32 * P.h.ld_scale;
-            // rows of this thread in the part, from r on; none where the row has no such column (rows are padded to 16 codes, so a
-            // chunk that begins inside is readable as a whole)
-            const int rows_left = col < P.No ? (int)min((long long)part.n * kBlockRows - r, P.R - row0) : 0;
-            uint4 w[kAhead][2];
-            uint32_t byte[kAhead][2];
-            int ahead = rows_left;                            // rows left from the k-block that is fetched next
-            const auto fetch = [&](uint4 (&fw)[2], uint32_t (&fb)[2]) {
-                const bool in0 = ahead > 0, in1 = ahead > 32;
-                fw[0] = in0 ? __ldg(reinterpret_cast<const uint4 *>(code)) : make_uint4(0u, 0u, 0u, 0u);
-                fb[0] = in0 ? __ldg(scale) : 0u;
-                fw[1] = in1 ? __ldg(reinterpret_cast<const uint4 *>(code + code_half)) : make_uint4(0u, 0u, 0u, 0u);
-                fb[1] = in1 ? __ldg(scale + scale_half) : 0u;
-                code += 2 * code_half;
-                scale += 2 * scale_half;
-                ahead -= kBlockRows;
+            // rows are padded to 16 codes, so eight that begin inside a row are readable as a whole; beyond it there is nothing
+            const bool in_cols = col < P.No;
+            const uint8_t *code = P.h.code + col, *scale = P.h.scale + (col >> 5);
+            const int ld_code = (int)P.h.ld_code, ld_scale = (int)P.h.ld_scale;
+            int row = part.k0 * kBlockRows + r;               // that is fetched next
+            int last_row = P.R - part.k0 * kBlockRows;        // the part's rows from the k-block on that is restored next
+            struct Batch { uint2 w[2 * kBatch]; uint32_t byte[2 * kBatch]; };
+            const auto fetch = [&](Batch &b) {
+                if (in_cols && row - r + kBatch * kBlockRows <= P.R) {
+#pragma unroll
+                    for (int q = 0; q < 2 * kBatch; ++q) {
+                        b.w[q] = load_codes(code + (long long)(row + 32 * q) * ld_code);
+                        b.byte[q] = load_byte(scale + (long long)(row + 32 * q) * ld_scale);
+                    }
+                } else {
+#pragma unroll
+                    for (int q = 0; q < 2 * kBatch; ++q) {
+                        const bool in = in_cols && row + 32 * q < P.R;
+                        b.w[q] = in ? load_codes(code + (long long)(row + 32 * q) * ld_code) : make_uint2(0u, 0u);
+                        b.byte[q] = in ? load_byte(scale + (long long)(row + 32 * q) * ld_scale) : 0u;
+                    }
+                }
+                row += kBatch * kBlockRows;
             };
+            const auto restore = [&](const Batch &b, int i0) {
 #pragma unroll
-            for (int d = 0; d < kAhead; ++d) fetch(w[d], byte[d]);
-            for (int i0 = 0; ok && i0 < part.n; i0 += kAhead) {
-#pragma unroll
-                for (int d = 0; d < kAhead; ++d) {
-                    const int i = i0 + d;
-                    if (i >= part.n) break;
-                    if (!(ok = __all_sync(0xffffffffu, mbar_wait(&empty[stage], phase ^ 1u, abort_flag)))) break;
-                    const uint32_t dst = smem_u32(tiles + (size_t)stage * PL::kStageBytes) + at;
+                for (int d = 0; d < kBatch; ++d) {
+                    if (i0 + d >= part.n) break;
+                    if (!__all_sync(0xffffffffu, ready) && !(ok = __all_sync(0xffffffffu, mbar_wait(&empty[stage], phase ^ 1u, abort_flag)))) break;
+                    const uint32_t dst = tile0 + (uint32_t)(stage * PL::kStageBytes), bar = full0 + (uint32_t)(stage * 8);
+                    if (++stage == PL::kStages) { stage = 0; phase ^= 1u; }
+                    ready = mbar_test(&empty[stage], phase ^ 1u);            // (the next stage: its answer is not waited for yet)
 #pragma unroll
                     for (int q = 0; q < 2; ++q) {
-                        uint32_t o[8];
-                        if (FORM == IM_ACT8_INT8 && byte[d][q] > 227u) restore16<FORM, MODE, true>(w[d][q], act8_scale(byte[d][q]), ga, be, o);
-                        else restore16<FORM, MODE, false>(w[d][q], __uint_as_float(byte[d][q] << 23), ga, be, o);
-                        if (FORM != IM_ACT8_INT8 && byte[d][q] == 255u) {
-#pragma unroll
-                            for (int c = 0; c < 8; ++c) o[c] = 0x7fc07fc0u;
-                        }
-                        if (MODE && i * kBlockRows + 32 * q >= rows_left) {                 // behind the last row: zeros, not beta
-#pragma unroll
-                            for (int c = 0; c < 8; ++c) o[c] = 0u;
-                        }
-                        asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(dst + q * 4096 + c0), "r"(o[0]), "r"(o[1]), "r"(o[2]), "r"(o[3]) : "memory");
-                        asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(dst + q * 4096 + c1), "r"(o[4]), "r"(o[5]), "r"(o[6]), "r"(o[7]) : "memory");
+                        uint32_t o[4];
+                        // (a marked block's byte, 255, is an infinity here, and its codes are 0: NaN)
+                        restore8<FORM, MODE>(b.w[2 * d + q], __uint_as_float(b.byte[2 * d + q] << 23), ga, be, o);
+                        if (MODE && last_row < kBlockRows && r + 32 * q >= last_row) o[0] = o[1] = o[2] = o[3] = 0u;   // behind the last row: zeros, not beta
+                        asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(dst + q * 4096), "r"(o[0]), "r"(o[1]), "r"(o[2]), "r"(o[3]) : "memory");
                     }
-                    fetch(w[d], byte[d]);
+                    last_row -= kBlockRows;
                     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                     __syncwarp();
                     if (lane == 0) {
-                        if (PAIR) mbar_arrive_leader(&full[stage]);
-                        else mbar_arrive(&full[stage]);
+                        if (PAIR) mbar_arrive_remote(bar);
+                        else mbar_arrive_addr(bar);
                     }
-                    if (++stage == PL::kStages) { stage = 0; phase ^= 1u; }
                 }
+            };
+            Batch even, odd;
+            fetch(even);
+            for (int i = 0; ok && i < part.n; i += 2 * kBatch) {
+                fetch(odd);
+                restore(even, i);
+                if (!ok || i + kBatch >= part.n) break;
+                fetch(even);
+                restore(odd, i + kBatch);
             }
         }
     } else {
@@ -326,30 +363,35 @@ __device__ __forceinline__ void act8_tn_body(const CUtensorMap &map_a, const Act
             for (int i0 = 0; i0 < part.n; i0 += kChainBlocks) {
                 if (!(ok = __all_sync(0xffffffffu, mbar_wait(&acc_full[acc], acc_phase, abort_flag)))) break;
                 tc_fence_after();
-                const uint32_t t_row = tmem_base + ((uint32_t)(quad * 32) << 16) + (uint32_t)(acc * BLOCK_N);
+                const uint32_t t_quad = tmem_base + ((uint32_t)(quad * 32) << 16), t_row = t_quad + (uint32_t)(acc * BLOCK_N), t_sum = t_quad + (uint32_t)(PL::kAccs * BLOCK_N);
+                // 32 columns at a time: the accumulator plus the sum so far, back into the sum, or out if it is the last chain
+                const bool first = i0 == 0, last = i0 + kChainBlocks >= part.n;
 #pragma unroll 1
                 for (int c0 = 0; c0 < BLOCK_N; c0 += 32) {
                     float v[32];
                     tmem_ld32_issue(t_row + (uint32_t)c0, v);
-                    tmem_ld_wait();
-                    float *p = dst + (long long)c0 * ld;
-                    if (i0 == 0) {
+                    if (!first) {
+                        float sum[32];
+                        tmem_ld32_issue(t_sum + (uint32_t)c0, sum);
+                        tmem_ld_wait();
+#pragma unroll
+                        for (int c = 0; c < 32; ++c) v[c] += sum[c];
+                    } else tmem_ld_wait();
+                    if (!last) tmem_st32(t_sum + (uint32_t)c0, v);
+                    else {
 #pragma unroll
                         for (int c = 0; c < 32; ++c)
-                            if (c0 + c < rows) p[(long long)c * ld] = v[c];
-                    } else {
-#pragma unroll
-                        for (int c = 0; c < 32; ++c)
-                            if (c0 + c < rows) asm volatile("red.relaxed.gpu.global.add.f32 [%0], %1;" ::"l"(p + (long long)c * ld), "f"(v[c]) : "memory");
+                            if (c0 + c < rows) dst[(long long)(c0 + c) * ld] = v[c];
                     }
                 }
+                if (!last) asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
                 tc_fence_before();
                 __syncwarp();
                 if (lane == 0) {
-                    if (PAIR) mbar_arrive_leader(&acc_empty[acc]);
+                    if (PAIR) mbar_arrive_remote(map_to_rank(smem_u32(&acc_empty[acc]), 0));
                     else mbar_arrive(&acc_empty[acc]);
                 }
-                if (++acc == 2) { acc = 0; acc_phase ^= 1u; }
+                if (++acc == PL::kAccs) { acc = 0; acc_phase ^= 1u; }
             }
         }
     }
@@ -498,7 +540,7 @@ im_status im_gemm_act8_tn(const uint16_t *A, int64_t lda, const im_act8 *H, floa
     using namespace im;
     if (!A || !C || !status || R < 1 || Mo < 1 || No < 1 || lda < Mo || ldc < No || (lda & 7) || !aligned_to(A, 16) || !aligned_to(C, 4)) return IM_ERR_INVALID_ARG;
     if (!act8_valid(H, No) || (H->ld_code & 15) || !aligned_to(H->code, 16)) return IM_ERR_INVALID_ARG;
-    if (Mo > kMaxCols || No > kMaxCols) return IM_ERR_UNSUPPORTED;
+    if (Mo > kMaxCols || No > kMaxCols || R > kMaxRows || H->ld_code > kMaxStride || H->ld_scale > kMaxStride) return IM_ERR_UNSUPPORTED;
     const size_t need = im_gemm_act8_tn_workspace_bytes(R, Mo, No);
     if (need && (!workspace || workspace_bytes < need || !aligned_to(workspace, 16))) return IM_ERR_INVALID_ARG;
     int n_sm = device_sm_count();
