@@ -1,10 +1,11 @@
 // Weight gradient from an 8-bit checkpoint: C[n][k] = sum over rows r of A[r][n] H[r][k], A bf16 (the gradient at a layer's
 // pre-activation), H restored from im_act8: code 2^e, or bf16(act(gamma code 2^e + beta)).  fp32 accumulation and output.
 //
-// Warp 0 fetches A's tiles by TMA (64 rows x 128-byte column blocks, 128B-swizzled), warps 2..17 restore H's tile (64 rows x
-// 128 columns) from global memory through registers into the layout that a swizzled TMA load would leave, warp 1 issues
-// tcgen05.mma on both as M/N-major operands, warps 18..21 take finished accumulators out of tensor memory.  H is the M
-// operand, so that a thread of the epilogue holds one k and its warp stores 32 neighbouring k of a row of C.
+// 28 warps: 0 fetches A's tiles by TMA (64 rows x 64-column blocks, 128B-swizzled), 1 issues tcgen05.mma, 2 fetches H's codes
+// (64 x 128, by TMA) and with 3 its scales (through registers, any alignment), 4..19 restore H's tile from shared memory into
+// the layout that a swizzled TMA load of bf16 would leave, 20..27 take finished accumulators out of tensor memory.  Both
+// operands are M/N-major; H is the M operand, so that a thread of the epilogue holds one k and its warp stores 32 neighbouring
+// k of a row of C.
 //
 // PAIR: two CTAs of a cluster compute 256 k x 256 n together (cta_group::2), each restoring its own 128 columns of H and
 // fetching half of A's columns: per k-block an SM takes in 16 KB of A and 8 KB of codes in place of 32 + 8 on a 128 x 256 tile of
@@ -32,13 +33,15 @@ namespace {
 
 constexpr int kTileK = 128;                // columns of H per CTA: the M of the instruction, or half of it
 constexpr int kBlockRows = 64;             // rows of a k-block
-constexpr int kDecodeWarps = 16, kEpiWarps = 4;
-constexpr int kThreads = 32 * (2 + kDecodeWarps + kEpiWarps);
+constexpr int kScaleWarps = 2, kDecodeWarps = 16, kEpiWarps = 8;
+constexpr int kFirstDecode = 2 + kScaleWarps, kFirstEpi = kFirstDecode + kDecodeWarps;
+constexpr int kThreads = 32 * (kFirstEpi + kEpiWarps);
 constexpr int kMaxCtas = 160;              // (the workspace is sized for so many)
 constexpr int kChainBlocks = 16;           // k-blocks accumulated in tensor memory before they are added in fp32
-constexpr int kBatch = 2;                  // k-blocks whose codes a restoring thread asks for together, a batch ahead
+constexpr int kRaw = 7;                    // k-blocks of codes and scales in flight
+constexpr int kRawBytes = kBlockRows * kTileK, kScaleBytes = kBlockRows * (kTileK / kActBlock);
 constexpr int kMaxCols = 65536;            // of either operand
-constexpr int kMaxRows = 0x7fff0000, kMaxStride = 0x7fffffff;               // row numbers (a k-block or two beyond the last) and strides of H in 32 bits
+constexpr int kMaxRows = 0x7fff0000;       // row numbers (a k-block beyond the last) in 32 bits
 constexpr size_t kSmemLimit = 232448;
 
 struct Act8GemmParams {
@@ -60,10 +63,11 @@ struct Plan {
     static constexpr int kCols = PAIR ? 2 * kTileK : kTileK;                     // columns of H per tile
     static constexpr int kACols = PAIR ? BLOCK_N / 2 : BLOCK_N;                  // columns of A that a CTA fetches
     static constexpr int kHBytes = kTileK * kBlockRows * 2, kABytes = kACols * kBlockRows * 2, kStageBytes = kHBytes + kABytes;
-    static constexpr int kStages = (int)((kSmemLimit - 2048) / kStageBytes) > 8 ? 8 : (int)((kSmemLimit - 2048) / kStageBytes);
+    static constexpr int kStages = BLOCK_N == 64 ? 6 : 5;
     static constexpr int kAccs = PAIR ? 1 : 2;                                   // accumulators; behind them the sum of finished chains
     static constexpr int kTmemCols = BLOCK_N == 64 ? 256 : 512;                  // at least (kAccs + 1) BLOCK_N, a power of two
-    static constexpr size_t kSmemBytes = 1024 + (size_t)kStages * kStageBytes + 512;
+    static constexpr size_t kSmemBytes = 1024 + (size_t)kStages * kStageBytes + (size_t)kRaw * (kRawBytes + kScaleBytes) + 512;
+    static_assert(kSmemBytes <= kSmemLimit && (2 * kStages + 2 * kRaw + 2 * kAccs + 1) * 8 <= 512, "shared memory plan");
 };
 
 // The k-blocks [k0, k0 + n) of a tile, one after another for a worker; slot: where their sum goes.
@@ -116,37 +120,37 @@ __device__ __forceinline__ void restore8(const uint2 &w, float scale, const F2 *
     }
 }
 
-// Loads that keep their place: the compiler would move them down to their first use.
-__device__ __forceinline__ uint2 load_codes(const uint8_t *p)
+// The scale bytes of the 128 columns from block b0 of a row on, as one word (blocks behind the last: 0).  Loads that keep their
+// place: the compiler would move them down to their first use.
+__device__ __forceinline__ uint32_t load_scales(const uint8_t *p, int blocks, bool word)
 {
-    uint2 w;
-    asm volatile("ld.global.nc.L1::no_allocate.v2.b32 {%0, %1}, [%2];" : "=r"(w.x), "=r"(w.y) : "l"(p));
+    uint32_t w = 0u;
+    if (word) {
+        asm volatile("ld.global.nc.b32 %0, [%1];" : "=r"(w) : "l"(p));
+        return w;
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+        if (i < blocks) {
+            uint32_t b;
+            asm volatile("ld.global.nc.u8 %0, [%1];" : "=r"(b) : "l"(p + i));
+            w |= b << (8 * i);
+        }
     return w;
 }
-__device__ __forceinline__ uint32_t load_byte(const uint8_t *p)
-{
-    uint32_t b;
-    asm volatile("ld.global.nc.u8 %0, [%1];" : "=r"(b) : "l"(p));
-    return b;
-}
-__device__ __forceinline__ bool mbar_test(uint64_t *bar, uint32_t parity)
-{
-    uint32_t ok;
-    asm volatile("{\n\t.reg .pred p;\n\tmbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}"
-                 : "=r"(ok) : "r"(smem_u32(bar)), "r"(parity) : "memory");
-    return ok != 0;
-}
-
-__device__ __forceinline__ void tmem_st32(uint32_t taddr, const float *v)
+__device__ __forceinline__ void tmem_st16(uint32_t taddr, const float (&v)[16])
 {
     const uint32_t *r = reinterpret_cast<const uint32_t *>(v);
-    asm volatile("tcgen05.st.sync.aligned.32x32b.x32.b32 [%32], "
-                 "{%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,"
-                 "%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31};"
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%16], {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15};"
                  ::"r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]),
-                   "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]),
-                   "r"(r[16]), "r"(r[17]), "r"(r[18]), "r"(r[19]), "r"(r[20]), "r"(r[21]), "r"(r[22]), "r"(r[23]),
-                   "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]), "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31]), "r"(taddr) : "memory");
+                   "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(taddr) : "memory");
+}
+__device__ __forceinline__ void tmem_ld16_issue(uint32_t taddr, float (&v)[16])
+{
+    uint32_t *r = reinterpret_cast<uint32_t *>(v);
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]),
+                   "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]) : "r"(taddr));
 }
 // One lane of a converged warp, the same every time.
 __device__ __forceinline__ bool elect_one()
@@ -166,24 +170,26 @@ __device__ __forceinline__ void mbar_arrive_remote(uint32_t cluster_addr)
 __device__ __forceinline__ void mbar_arrive_addr(uint32_t addr) { asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(addr) : "memory"); }
 
 template <int BLOCK_N, bool PAIR, int FORM, int MODE>
-__device__ __forceinline__ void act8_tn_body(const CUtensorMap &map_a, const Act8GemmParams &P)
+__device__ __forceinline__ void act8_tn_body(const CUtensorMap &map_a, const CUtensorMap &map_h, const Act8GemmParams &P)
 {
     using PL = Plan<BLOCK_N, PAIR>;
     extern __shared__ uint8_t smem_raw[];
     uint8_t *tiles = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
-    uint64_t *full = reinterpret_cast<uint64_t *>(tiles + (size_t)PL::kStages * PL::kStageBytes);
-    uint64_t *empty = full + PL::kStages, *acc_full = empty + PL::kStages, *acc_empty = acc_full + 2;
-    uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(acc_empty + 2);
+    uint8_t *raw = tiles + (size_t)PL::kStages * PL::kStageBytes, *scales = raw + (size_t)kRaw * kRawBytes;
+    uint64_t *full = reinterpret_cast<uint64_t *>(scales + (size_t)kRaw * kScaleBytes);
+    uint64_t *empty = full + PL::kStages, *raw_full = empty + PL::kStages, *raw_empty = raw_full + kRaw, *acc_full = raw_empty + kRaw, *acc_empty = acc_full + PL::kAccs;
+    uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(acc_empty + PL::kAccs);
     volatile int *abort_flag = reinterpret_cast<volatile int *>(tmem_slot + 1);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const uint32_t rank = PAIR ? cluster_rank() : 0u;
     const int worker = PAIR ? (int)blockIdx.x >> 1 : (int)blockIdx.x;
     constexpr int kCtas = PAIR ? 2 : 1;
 
-    // full, acc_empty: of the pair's leader (rank 0), whose MMA thread waits on them; empty, acc_full: each CTA's own
+    // full, acc_empty: of the pair's leader (rank 0), whose MMA warp waits on them; the others: each CTA's own
     if (threadIdx.x == 0) {
         for (int s = 0; s < PL::kStages; ++s) { mbar_init(&full[s], 1 + kCtas * kDecodeWarps); mbar_init(&empty[s], 1); }
-        for (int a = 0; a < 2; ++a) { mbar_init(&acc_full[a], 1); mbar_init(&acc_empty[a], kCtas * kEpiWarps); }
+        for (int q = 0; q < kRaw; ++q) { mbar_init(&raw_full[q], 1 + kScaleWarps); mbar_init(&raw_empty[q], kDecodeWarps); }
+        for (int a = 0; a < PL::kAccs; ++a) { mbar_init(&acc_full[a], 1); mbar_init(&acc_empty[a], kCtas * kEpiWarps); }
         *abort_flag = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
@@ -272,15 +278,54 @@ __device__ __forceinline__ void act8_tn_body(const CUtensorMap &map_a, const Act
                 }
             }
         }
-    } else if (warp < 2 + kDecodeWarps) {
+    } else if (warp < kFirstDecode) {
+        // codes (warp 2) and scales (a row per lane; words are asked for kLead k-blocks ahead)
+        constexpr int kLead = 4;
+        const bool one = warp == 2 && elect_one();
+        const int r = (warp - 2) * 32 + lane;
+        int slot = 0;
+        if (!g_skip_loads)
+            for (int j = 0; ok && part_at(P, worker, j, part); ++j) {
+                const int col = (part.tile % P.tiles_k) * PL::kCols + (int)rank * kTileK, blocks = (P.No - col + kActBlock - 1) / kActBlock;
+                const bool word = blocks >= 4 && ((reinterpret_cast<uintptr_t>(P.h.scale) | (uintptr_t)P.h.ld_scale) & 3u) == 0;
+                const uint8_t *p = P.h.scale + (col >> 5);
+                int row = part.k0 * kBlockRows + r;                              // of the next word asked for
+                uint32_t w[kLead];
+                const auto ask = [&](uint32_t &to) {
+                    to = row < P.R ? load_scales(p + (long long)row * P.h.ld_scale, blocks, word) : 0u;
+                    row += kBlockRows;
+                };
+#pragma unroll
+                for (int d = 0; d < kLead; ++d) ask(w[d]);
+                for (int i0 = 0; ok && i0 < part.n; i0 += kLead) {
+#pragma unroll
+                    for (int d = 0; d < kLead; ++d) {
+                        if (i0 + d >= part.n) break;
+                        if (!(ok = __all_sync(0xffffffffu, mbar_wait(&raw_empty[slot], phase ^ 1u, abort_flag)))) break;
+                        if (one) {
+                            mbar_arrive_expect_tx(&raw_full[slot], kRawBytes);
+                            tma_load_2d(raw + (size_t)slot * kRawBytes, &map_h, &raw_full[slot], col, (part.k0 + i0 + d) * kBlockRows);
+                        }
+                        reinterpret_cast<uint32_t *>(scales + (size_t)slot * kScaleBytes)[r] = w[d];
+                        __syncwarp();
+                        if (lane == 0) mbar_arrive(&raw_full[slot]);
+                        ask(w[d]);
+                        if (++slot == kRaw) { slot = 0; phase ^= 1u; }
+                    }
+                }
+            }
+    } else if (warp < kFirstEpi) {
         // thread: 8 neighbouring columns of rows r and r + 32 of every k-block.  Eight lanes cover the 64 columns of a swizzled block
-        // row, so that a 16-byte store phase meets all banks; with 8 columns gamma and beta take 16 registers, which leaves room
-        // for the 16 warps that hide the latencies of loads, barriers and conversions.  Codes are asked for in batches, a batch
-        // ahead: one wait for all loads of a batch.
-        const int tid = (warp - 2) * 32 + lane, half = tid >> 8, cq = tid & 7, r = (tid >> 3) & 31;
+        // row, so that a 16-byte store phase meets all banks; the four rows of a warp are b, b + 4, b + 1, b + 5, so that the two
+        // rows of a half warp lie in different halves of the codes' swizzle.
+        const int tid = (warp - kFirstDecode) * 32 + lane, half = tid >> 8, cq = tid & 7, w8 = (tid >> 5) & 7, l4 = (tid >> 3) & 3;
+        const int r = (w8 >> 1) * 8 + (w8 & 1) * 2 + (l4 & 1) * 4 + (l4 >> 1);
         const uint32_t tile0 = smem_u32(tiles) + (uint32_t)(half * 8192 + r * 128) + (uint32_t)((cq ^ (r & 7)) << 4);
+        const uint32_t raw0 = smem_u32(raw) + (uint32_t)(r * 128) + (uint32_t)(((half * 4 + (cq >> 1)) ^ (r & 7)) << 4) + (uint32_t)((cq & 1) * 8);
+        const uint32_t scale0 = smem_u32(scales) + (uint32_t)(r * 4 + half * 2 + (cq >> 2));
         const uint32_t full0 = PAIR ? map_to_rank(smem_u32(full), 0) : smem_u32(full);
-        bool ready = mbar_test(&empty[0], 1u);
+        int slot = 0;
+        uint32_t raw_phase = 0;
         for (int j = 0; ok && part_at(P, worker, j, part); ++j) {
             const int col = (part.tile % P.tiles_k) * PL::kCols + (int)rank * kTileK + half * 64 + cq * 8;
             F2 ga[MODE ? 4 : 1], be[MODE ? 4 : 1];
@@ -292,67 +337,42 @@ __device__ __forceinline__ void act8_tn_body(const CUtensorMap &map_a, const Act
                     be[c] = f2(at_col(P.beta, col + 2 * c, 0.0f), at_col(P.beta, col + 2 * c + 1, 0.0f));
                 }
             }
-            // rows are padded to 16 codes, so eight that begin inside a row are readable as a whole; beyond it there is nothing
-            const bool in_cols = col < P.No;
-            const uint8_t *code = P.h.code + col, *scale = P.h.scale + (col >> 5);
-            const int ld_code = (int)P.h.ld_code, ld_scale = (int)P.h.ld_scale;
-            int row = part.k0 * kBlockRows + r;               // that is fetched next
-            int last_row = P.R - part.k0 * kBlockRows;        // the part's rows from the k-block on that is restored next
-            struct Batch { uint2 w[2 * kBatch]; uint32_t byte[2 * kBatch]; };
-            const auto fetch = [&](Batch &b) {
-                if (in_cols && row - r + kBatch * kBlockRows <= P.R) {
+            int rows_left = P.R - part.k0 * kBlockRows;         // from this k-block on
+            for (int i = 0; i < part.n; ++i, rows_left -= kBlockRows) {
+                if (!(ok = __all_sync(0xffffffffu, mbar_wait(&raw_full[slot], raw_phase, abort_flag)))) break;
+                uint2 w[2];
+                uint32_t byte[2];
 #pragma unroll
-                    for (int q = 0; q < 2 * kBatch; ++q) {
-                        b.w[q] = load_codes(code + (long long)(row + 32 * q) * ld_code);
-                        b.byte[q] = load_byte(scale + (long long)(row + 32 * q) * ld_scale);
-                    }
-                } else {
-#pragma unroll
-                    for (int q = 0; q < 2 * kBatch; ++q) {
-                        const bool in = in_cols && row + 32 * q < P.R;
-                        b.w[q] = in ? load_codes(code + (long long)(row + 32 * q) * ld_code) : make_uint2(0u, 0u);
-                        b.byte[q] = in ? load_byte(scale + (long long)(row + 32 * q) * ld_scale) : 0u;
-                    }
+                for (int q = 0; q < 2; ++q) {
+                    asm volatile("ld.shared.v2.b32 {%0, %1}, [%2];" : "=r"(w[q].x), "=r"(w[q].y) : "r"(raw0 + (uint32_t)(slot * kRawBytes + q * 4096)) : "memory");
+                    asm volatile("ld.shared.u8 %0, [%1];" : "=r"(byte[q]) : "r"(scale0 + (uint32_t)(slot * kScaleBytes + q * 128)) : "memory");
                 }
-                row += kBatch * kBlockRows;
-            };
-            const auto restore = [&](const Batch &b, int i0) {
+                uint32_t o[2][4];
 #pragma unroll
-                for (int d = 0; d < kBatch; ++d) {
-                    if (i0 + d >= part.n) break;
-                    if (!__all_sync(0xffffffffu, ready) && !(ok = __all_sync(0xffffffffu, mbar_wait(&empty[stage], phase ^ 1u, abort_flag)))) break;
-                    const uint32_t dst = tile0 + (uint32_t)(stage * PL::kStageBytes), bar = full0 + (uint32_t)(stage * 8);
-                    if (++stage == PL::kStages) { stage = 0; phase ^= 1u; }
-                    ready = mbar_test(&empty[stage], phase ^ 1u);            // (the next stage: its answer is not waited for yet)
-#pragma unroll
-                    for (int q = 0; q < 2; ++q) {
-                        uint32_t o[4];
-                        // (a marked block's byte, 255, is an infinity here, and its codes are 0: NaN)
-                        restore8<FORM, MODE>(b.w[2 * d + q], __uint_as_float(b.byte[2 * d + q] << 23), ga, be, o);
-                        if (MODE && last_row < kBlockRows && r + 32 * q >= last_row) o[0] = o[1] = o[2] = o[3] = 0u;   // behind the last row: zeros, not beta
-                        asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(dst + q * 4096), "r"(o[0]), "r"(o[1]), "r"(o[2]), "r"(o[3]) : "memory");
-                    }
-                    last_row -= kBlockRows;
-                    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-                    __syncwarp();
-                    if (lane == 0) {
-                        if (PAIR) mbar_arrive_remote(bar);
-                        else mbar_arrive_addr(bar);
-                    }
+                for (int q = 0; q < 2; ++q) {
+                    // (a marked block's byte, 255, is an infinity here, and its codes are 0: NaN)
+                    restore8<FORM, MODE>(w[q], __uint_as_float(byte[q] << 23), ga, be, o[q]);
+                    if (MODE && rows_left < kBlockRows && r + 32 * q >= rows_left) o[q][0] = o[q][1] = o[q][2] = o[q][3] = 0u;   // behind the last row: zeros, not beta
                 }
-            };
-            Batch even, odd;
-            fetch(even);
-            for (int i = 0; ok && i < part.n; i += 2 * kBatch) {
-                fetch(odd);
-                restore(even, i);
-                if (!ok || i + kBatch >= part.n) break;
-                fetch(even);
-                restore(odd, i + kBatch);
+                if (!(ok = __all_sync(0xffffffffu, mbar_wait(&empty[stage], phase ^ 1u, abort_flag)))) break;
+#pragma unroll
+                for (int q = 0; q < 2; ++q)
+                    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(tile0 + (uint32_t)(stage * PL::kStageBytes + q * 4096)), "r"(o[q][0]), "r"(o[q][1]),
+                                 "r"(o[q][2]), "r"(o[q][3]) : "memory");
+                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                __syncwarp();
+                if (lane == 0) {
+                    mbar_arrive(&raw_empty[slot]);
+                    if (PAIR) mbar_arrive_remote(full0 + (uint32_t)(stage * 8));
+                    else mbar_arrive_addr(full0 + (uint32_t)(stage * 8));
+                }
+                if (++stage == PL::kStages) { stage = 0; phase ^= 1u; }
+                if (++slot == kRaw) { slot = 0; raw_phase ^= 1u; }
             }
         }
     } else {
-        const int quad = warp & 3;                         // tensor-memory lanes 32 quad .. 32 quad + 31
+        // two warps per quadrant of tensor memory (lanes 32 quad .. 32 quad + 31), each with one half of the tile's columns
+        const int quad = warp & 3, c_first = ((warp - kFirstEpi) >> 2) * (BLOCK_N / 2);
         for (int j = 0; ok && part_at(P, worker, j, part); ++j) {
             const int n0 = part.tile / P.tiles_k * BLOCK_N, in_tile = (int)rank * kTileK + quad * 32 + lane;
             const int k = (part.tile % P.tiles_k) * PL::kCols + in_tile;
@@ -364,23 +384,22 @@ __device__ __forceinline__ void act8_tn_body(const CUtensorMap &map_a, const Act
                 if (!(ok = __all_sync(0xffffffffu, mbar_wait(&acc_full[acc], acc_phase, abort_flag)))) break;
                 tc_fence_after();
                 const uint32_t t_quad = tmem_base + ((uint32_t)(quad * 32) << 16), t_row = t_quad + (uint32_t)(acc * BLOCK_N), t_sum = t_quad + (uint32_t)(PL::kAccs * BLOCK_N);
-                // 32 columns at a time: the accumulator plus the sum so far, back into the sum, or out if it is the last chain
+                // 16 columns at a time: the accumulator plus the sum so far, back into the sum, or out if it is the last chain
                 const bool first = i0 == 0, last = i0 + kChainBlocks >= part.n;
-#pragma unroll 1
-                for (int c0 = 0; c0 < BLOCK_N; c0 += 32) {
-                    float v[32];
-                    tmem_ld32_issue(t_row + (uint32_t)c0, v);
+#pragma unroll 2
+                for (int c0 = c_first; c0 < c_first + BLOCK_N / 2; c0 += 16) {
+                    float v[16], sum[16];
+                    tmem_ld16_issue(t_row + (uint32_t)c0, v);
+                    if (!first) tmem_ld16_issue(t_sum + (uint32_t)c0, sum);
+                    tmem_ld_wait();
                     if (!first) {
-                        float sum[32];
-                        tmem_ld32_issue(t_sum + (uint32_t)c0, sum);
-                        tmem_ld_wait();
 #pragma unroll
-                        for (int c = 0; c < 32; ++c) v[c] += sum[c];
-                    } else tmem_ld_wait();
-                    if (!last) tmem_st32(t_sum + (uint32_t)c0, v);
+                        for (int c = 0; c < 16; ++c) v[c] += sum[c];
+                    }
+                    if (!last) tmem_st16(t_sum + (uint32_t)c0, v);
                     else {
 #pragma unroll
-                        for (int c = 0; c < 32; ++c)
+                        for (int c = 0; c < 16; ++c)
                             if (c0 + c < rows) dst[(long long)(c0 + c) * ld] = v[c];
                     }
                 }
@@ -412,14 +431,16 @@ __device__ __forceinline__ void act8_tn_body(const CUtensorMap &map_a, const Act
     }
 }
 template <int BLOCK_N, int FORM, int MODE>
-__global__ void __launch_bounds__(kThreads, 1) act8_tn_kernel(const __grid_constant__ CUtensorMap map_a, const Act8GemmParams P)
+__global__ void __launch_bounds__(kThreads, 1) act8_tn_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_h,
+                                                              const Act8GemmParams P)
 {
-    act8_tn_body<BLOCK_N, false, FORM, MODE>(map_a, P);
+    act8_tn_body<BLOCK_N, false, FORM, MODE>(map_a, map_h, P);
 }
 template <int FORM, int MODE>
-__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) act8_tn_pair_kernel(const __grid_constant__ CUtensorMap map_a, const Act8GemmParams P)
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) act8_tn_pair_kernel(const __grid_constant__ CUtensorMap map_a,
+                                                                                            const __grid_constant__ CUtensorMap map_h, const Act8GemmParams P)
 {
-    act8_tn_body<256, true, FORM, MODE>(map_a, P);
+    act8_tn_body<256, true, FORM, MODE>(map_a, map_h, P);
 }
 
 // C = the partial tiles, added in a fixed order (slices, then helpers): a warp per 128 columns of one row.
@@ -488,7 +509,7 @@ Split split_for(int R, int Mo, int No, int ctas)
 }
 
 template <int FORM, int MODE>
-cudaError_t launch_product(const Split &s, const CUtensorMap &map, const Act8GemmParams &p, int grid, cudaStream_t st)
+cudaError_t launch_product(const Split &s, const CUtensorMap &map, const CUtensorMap &map_h, const Act8GemmParams &p, int grid, cudaStream_t st)
 {
     static DeviceOnce once;
     const auto k64 = act8_tn_kernel<64, FORM, MODE>, k128 = act8_tn_kernel<128, FORM, MODE>, kpair = act8_tn_pair_kernel<FORM, MODE>;
@@ -499,16 +520,16 @@ cudaError_t launch_product(const Split &s, const CUtensorMap &map, const Act8Gem
         return r;
     });
     if (e != cudaSuccess) return e;
-    if (s.pair) kpair<<<grid, kThreads, Plan<256, true>::kSmemBytes, st>>>(map, p);
-    else if (s.block_n == 64) k64<<<grid, kThreads, Plan<64, false>::kSmemBytes, st>>>(map, p);
-    else k128<<<grid, kThreads, Plan<128, false>::kSmemBytes, st>>>(map, p);
+    if (s.pair) kpair<<<grid, kThreads, Plan<256, true>::kSmemBytes, st>>>(map, map_h, p);
+    else if (s.block_n == 64) k64<<<grid, kThreads, Plan<64, false>::kSmemBytes, st>>>(map, map_h, p);
+    else k128<<<grid, kThreads, Plan<128, false>::kSmemBytes, st>>>(map, map_h, p);
     return cudaGetLastError();
 }
 template <int FORM>
-cudaError_t launch_product(const Split &s, const CUtensorMap &map, const Act8GemmParams &p, int mode, int grid, cudaStream_t st)
+cudaError_t launch_product(const Split &s, const CUtensorMap &map, const CUtensorMap &map_h, const Act8GemmParams &p, int mode, int grid, cudaStream_t st)
 {
-    return mode == 0 ? launch_product<FORM, 0>(s, map, p, grid, st)
-         : mode == 1 ? launch_product<FORM, 1>(s, map, p, grid, st) : launch_product<FORM, 2>(s, map, p, grid, st);
+    return mode == 0 ? launch_product<FORM, 0>(s, map, map_h, p, grid, st)
+         : mode == 1 ? launch_product<FORM, 1>(s, map, map_h, p, grid, st) : launch_product<FORM, 2>(s, map, map_h, p, grid, st);
 }
 
 }  // namespace
@@ -540,14 +561,16 @@ im_status im_gemm_act8_tn(const uint16_t *A, int64_t lda, const im_act8 *H, floa
     using namespace im;
     if (!A || !C || !status || R < 1 || Mo < 1 || No < 1 || lda < Mo || ldc < No || (lda & 7) || !aligned_to(A, 16) || !aligned_to(C, 4)) return IM_ERR_INVALID_ARG;
     if (!act8_valid(H, No) || (H->ld_code & 15) || !aligned_to(H->code, 16)) return IM_ERR_INVALID_ARG;
-    if (Mo > kMaxCols || No > kMaxCols || R > kMaxRows || H->ld_code > kMaxStride || H->ld_scale > kMaxStride) return IM_ERR_UNSUPPORTED;
+    if (Mo > kMaxCols || No > kMaxCols || R > kMaxRows) return IM_ERR_UNSUPPORTED;
     const size_t need = im_gemm_act8_tn_workspace_bytes(R, Mo, No);
     if (need && (!workspace || workspace_bytes < need || !aligned_to(workspace, 16))) return IM_ERR_INVALID_ARG;
     int n_sm = device_sm_count();
     if (n_sm <= 0) return IM_ERR_UNSUPPORTED;
     n_sm = n_sm < kMaxCtas ? n_sm : kMaxCtas;
-    CUtensorMap map;
-    if (!make_map(&map, A, (uint64_t)R, (uint64_t)Mo, (uint64_t)lda, kBlockRows)) return IM_ERR_CUDA;
+    CUtensorMap map, map_h;
+    if (!make_map(&map, A, (uint64_t)R, (uint64_t)Mo, (uint64_t)lda, kBlockRows) ||
+        !make_map_bytes(&map_h, H->code, (uint64_t)R, (uint64_t)No, (uint64_t)H->ld_code, kBlockRows))
+        return IM_ERR_CUDA;
     const Split s = split_for(R, Mo, No, n_sm);
     Act8GemmParams p;
     std::memset(&p, 0, sizeof(p));
@@ -559,7 +582,7 @@ im_status im_gemm_act8_tn(const uint16_t *A, int64_t lda, const im_act8 *H, floa
     const int busy = s.helpers || s.tiles * s.slices >= s.workers ? s.workers : s.tiles * s.slices;
     const int grid = s.pair ? 2 * busy : busy;
     cudaStream_t st = (cudaStream_t)cuda_stream;
-    cudaError_t e = H->form == IM_ACT8_INT8 ? launch_product<IM_ACT8_INT8>(s, map, p, mode, grid, st) : launch_product<IM_ACT8_E4M3>(s, map, p, mode, grid, st);
+    cudaError_t e = H->form == IM_ACT8_INT8 ? launch_product<IM_ACT8_INT8>(s, map, map_h, p, mode, grid, st) : launch_product<IM_ACT8_E4M3>(s, map, map_h, p, mode, grid, st);
     g_launches.fetch_add(1, std::memory_order_relaxed);
     if (e == cudaSuccess && p.partial) {
         const dim3 fin((unsigned)((No + 127) / 128), (unsigned)((Mo + 7) / 8));
