@@ -152,6 +152,25 @@ __device__ __forceinline__ void tmem_ld16_issue(uint32_t taddr, float (&v)[16])
                  : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]),
                    "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]) : "r"(taddr));
 }
+// Bounded wait of a whole warp (the same answer in every lane): false when the limit ran out or another role gave up.  The hint lets
+// the hardware hold the warp for up to 20 us at a time: warps that spin take issue slots from those that restore.
+__device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity, volatile int *abort_flag)
+{
+    const auto try_once = [&]() {
+        uint32_t ok;
+        asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\n\tselp.u32 %0, 1, 0, p;\n\t}"
+                     : "=r"(ok) : "r"(bar), "r"(parity), "r"(20000u) : "memory");
+        return __all_sync(0xffffffffu, ok != 0);
+    };
+    if (try_once()) return true;
+    const unsigned long long t0 = global_ns();
+    for (;;) {
+        if (try_once()) return true;
+        const bool late = global_ns() - t0 > g_wait_limit_ns;
+        if (late) *abort_flag = 1;
+        if (__any_sync(0xffffffffu, late || *abort_flag)) return false;
+    }
+}
 // One lane of a converged warp, the same every time.
 __device__ __forceinline__ bool elect_one()
 {
@@ -224,7 +243,7 @@ __device__ __forceinline__ void act8_tn_body(const CUtensorMap &map_a, const CUt
                 const int n0 = part.tile / P.tiles_k * BLOCK_N + (int)rank * PL::kACols;
                 int row = part.k0 * kBlockRows;
                 for (int i = 0; i < part.n; ++i, row += kBlockRows) {
-                    if (!(ok = __all_sync(0xffffffffu, mbar_wait(&empty[stage], phase ^ 1u, abort_flag)))) break;
+                    if (!(ok = warp_wait(smem_u32(&empty[stage]), phase ^ 1u, abort_flag))) break;
                     uint8_t *sb = tiles + (size_t)stage * PL::kStageBytes + PL::kHBytes;
                     if (one) {
                         if (rank == 0) mbar_arrive_expect_tx(&full[stage], kCtas * PL::kABytes);
@@ -247,9 +266,9 @@ __device__ __forceinline__ void act8_tn_body(const CUtensorMap &map_a, const CUt
                 int in_chain = 0;
                 for (int i = 0; i < part.n; ++i) {
                     if (in_chain == 0) {
-                        if (!(ok = __all_sync(0xffffffffu, mbar_wait(&acc_empty[acc], acc_phase ^ 1u, abort_flag)))) break;
+                        if (!(ok = warp_wait(smem_u32(&acc_empty[acc]), acc_phase ^ 1u, abort_flag))) break;
                     }
-                    if (!(ok = __all_sync(0xffffffffu, mbar_wait(&full[stage], phase, abort_flag)))) break;
+                    if (!(ok = warp_wait(smem_u32(&full[stage]), phase, abort_flag))) break;
                     tc_fence_after();
                     const uint32_t d = tmem_base + (uint32_t)(acc * BLOCK_N);
                     const uint64_t step = (uint64_t)(uint32_t)(stage * (PL::kStageBytes >> 4)), dh = dh0 + step, da = da0 + step;
@@ -301,7 +320,7 @@ __device__ __forceinline__ void act8_tn_body(const CUtensorMap &map_a, const CUt
 #pragma unroll
                     for (int d = 0; d < kLead; ++d) {
                         if (i0 + d >= part.n) break;
-                        if (!(ok = __all_sync(0xffffffffu, mbar_wait(&raw_empty[slot], phase ^ 1u, abort_flag)))) break;
+                        if (!(ok = warp_wait(smem_u32(&raw_empty[slot]), phase ^ 1u, abort_flag))) break;
                         if (one) {
                             mbar_arrive_expect_tx(&raw_full[slot], kRawBytes);
                             tma_load_2d(raw + (size_t)slot * kRawBytes, &map_h, &raw_full[slot], col, (part.k0 + i0 + d) * kBlockRows);
@@ -339,7 +358,7 @@ __device__ __forceinline__ void act8_tn_body(const CUtensorMap &map_a, const CUt
             }
             int rows_left = P.R - part.k0 * kBlockRows;         // from this k-block on
             for (int i = 0; i < part.n; ++i, rows_left -= kBlockRows) {
-                if (!(ok = __all_sync(0xffffffffu, mbar_wait(&raw_full[slot], raw_phase, abort_flag)))) break;
+                if (!(ok = warp_wait(smem_u32(&raw_full[slot]), raw_phase, abort_flag))) break;
                 uint2 w[2];
                 uint32_t byte[2];
 #pragma unroll
@@ -354,7 +373,7 @@ __device__ __forceinline__ void act8_tn_body(const CUtensorMap &map_a, const CUt
                     restore8<FORM, MODE>(w[q], __uint_as_float(byte[q] << 23), ga, be, o[q]);
                     if (MODE && rows_left < kBlockRows && r + 32 * q >= rows_left) o[q][0] = o[q][1] = o[q][2] = o[q][3] = 0u;   // behind the last row: zeros, not beta
                 }
-                if (!(ok = __all_sync(0xffffffffu, mbar_wait(&empty[stage], phase ^ 1u, abort_flag)))) break;
+                if (!(ok = warp_wait(smem_u32(&empty[stage]), phase ^ 1u, abort_flag))) break;
 #pragma unroll
                 for (int q = 0; q < 2; ++q)
                     asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(tile0 + (uint32_t)(stage * PL::kStageBytes + q * 4096)), "r"(o[q][0]), "r"(o[q][1]),
@@ -381,7 +400,7 @@ __device__ __forceinline__ void act8_tn_body(const CUtensorMap &map_a, const CUt
             const long long ld = P.partial ? PL::kCols : P.ldc;
             const int rows = k < P.No ? min(BLOCK_N, P.Mo - n0) : 0;
             for (int i0 = 0; i0 < part.n; i0 += kChainBlocks) {
-                if (!(ok = __all_sync(0xffffffffu, mbar_wait(&acc_full[acc], acc_phase, abort_flag)))) break;
+                if (!(ok = warp_wait(smem_u32(&acc_full[acc]), acc_phase, abort_flag))) break;
                 tc_fence_after();
                 const uint32_t t_quad = tmem_base + ((uint32_t)(quad * 32) << 16), t_row = t_quad + (uint32_t)(acc * BLOCK_N), t_sum = t_quad + (uint32_t)(PL::kAccs * BLOCK_N);
                 // 16 columns at a time: the accumulator plus the sum so far, back into the sum, or out if it is the last chain
