@@ -33,12 +33,11 @@ namespace {
 
 constexpr int kTileK = 128;                // columns of H per CTA: the M of the instruction, or half of it
 constexpr int kBlockRows = 64;             // rows of a k-block
-constexpr int kScaleWarps = 2, kDecodeWarps = 16, kEpiWarps = 8;
+constexpr int kScaleWarps = 2, kDecodeWarps = 16, kGroupWarps = 8, kEpiWarps = 8;   // restoring warps: two groups, k-blocks in turn
 constexpr int kFirstDecode = 2 + kScaleWarps, kFirstEpi = kFirstDecode + kDecodeWarps;
 constexpr int kThreads = 32 * (kFirstEpi + kEpiWarps);
 constexpr int kMaxCtas = 160;              // (the workspace is sized for so many)
-constexpr int kChainBlocks = 16;           // k-blocks accumulated in tensor memory before they are added in fp32
-constexpr int kRaw = 7;                    // k-blocks of codes and scales in flight
+constexpr int kChainBlocks = 20;           // k-blocks accumulated in tensor memory before they are added in fp32
 constexpr int kRawBytes = kBlockRows * kTileK, kScaleBytes = kBlockRows * (kTileK / kActBlock);
 constexpr int kMaxCols = 65536;            // of either operand
 constexpr int kMaxRows = 0x7fff0000;       // row numbers (a k-block beyond the last) in 32 bits
@@ -62,12 +61,12 @@ template <int BLOCK_N, bool PAIR>
 struct Plan {
     static constexpr int kCols = PAIR ? 2 * kTileK : kTileK;                     // columns of H per tile
     static constexpr int kACols = PAIR ? BLOCK_N / 2 : BLOCK_N;                  // columns of A that a CTA fetches
-    static constexpr int kHBytes = kTileK * kBlockRows * 2, kABytes = kACols * kBlockRows * 2, kStageBytes = kHBytes + kABytes;
+    static constexpr int kHBytes = kTileK * kBlockRows * 2, kABytes = kACols * kBlockRows * 2, kStageBytes = kHBytes + kABytes;    // (and codes and scales elsewhere)
     static constexpr int kStages = BLOCK_N == 64 ? 6 : 5;
     static constexpr int kAccs = PAIR ? 1 : 2;                                   // accumulators; behind them the sum of finished chains
     static constexpr int kTmemCols = BLOCK_N == 64 ? 256 : 512;                  // at least (kAccs + 1) BLOCK_N, a power of two
-    static constexpr size_t kSmemBytes = 1024 + (size_t)kStages * kStageBytes + (size_t)kRaw * (kRawBytes + kScaleBytes) + 512;
-    static_assert(kSmemBytes <= kSmemLimit && (2 * kStages + 2 * kRaw + 2 * kAccs + 1) * 8 <= 512, "shared memory plan");
+    static constexpr size_t kSmemBytes = 1024 + (size_t)kStages * (kStageBytes + kRawBytes + kScaleBytes) + 512;
+    static_assert(kSmemBytes <= kSmemLimit && (4 * kStages + 2 * kAccs + 1) * 8 <= 512, "shared memory plan");
 };
 
 // The k-blocks [k0, k0 + n) of a tile, one after another for a worker; slot: where their sum goes.
@@ -138,12 +137,16 @@ __device__ __forceinline__ uint32_t load_scales(const uint8_t *p, int blocks, bo
         }
     return w;
 }
-__device__ __forceinline__ void tmem_st16(uint32_t taddr, const float (&v)[16])
+__device__ __forceinline__ void tmem_st32(uint32_t taddr, const float (&v)[32])
 {
     const uint32_t *r = reinterpret_cast<const uint32_t *>(v);
-    asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%16], {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15};"
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x32.b32 [%32], "
+                 "{%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,"
+                 "%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31};"
                  ::"r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]),
-                   "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(taddr) : "memory");
+                   "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]),
+                   "r"(r[16]), "r"(r[17]), "r"(r[18]), "r"(r[19]), "r"(r[20]), "r"(r[21]), "r"(r[22]), "r"(r[23]),
+                   "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]), "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31]), "r"(taddr) : "memory");
 }
 __device__ __forceinline__ void tmem_ld16_issue(uint32_t taddr, float (&v)[16])
 {
@@ -158,9 +161,9 @@ __device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity, volatil
 {
     const auto try_once = [&]() {
         uint32_t ok;
-        asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\n\tselp.u32 %0, 1, 0, p;\n\t}"
+        asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\n\tvote.sync.all.pred p, p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}"
                      : "=r"(ok) : "r"(bar), "r"(parity), "r"(20000u) : "memory");
-        return __all_sync(0xffffffffu, ok != 0);
+        return ok != 0;
     };
     if (try_once()) return true;
     const unsigned long long t0 = global_ns();
@@ -194,9 +197,9 @@ __device__ __forceinline__ void act8_tn_body(const CUtensorMap &map_a, const CUt
     using PL = Plan<BLOCK_N, PAIR>;
     extern __shared__ uint8_t smem_raw[];
     uint8_t *tiles = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
-    uint8_t *raw = tiles + (size_t)PL::kStages * PL::kStageBytes, *scales = raw + (size_t)kRaw * kRawBytes;
-    uint64_t *full = reinterpret_cast<uint64_t *>(scales + (size_t)kRaw * kScaleBytes);
-    uint64_t *empty = full + PL::kStages, *raw_full = empty + PL::kStages, *raw_empty = raw_full + kRaw, *acc_full = raw_empty + kRaw, *acc_empty = acc_full + PL::kAccs;
+    uint8_t *raw = tiles + (size_t)PL::kStages * PL::kStageBytes, *scales = raw + (size_t)PL::kStages * kRawBytes;
+    uint64_t *full = reinterpret_cast<uint64_t *>(scales + (size_t)PL::kStages * kScaleBytes);
+    uint64_t *empty = full + PL::kStages, *raw_full = empty + PL::kStages, *raw_empty = raw_full + PL::kStages, *acc_full = raw_empty + PL::kStages, *acc_empty = acc_full + PL::kAccs;
     uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(acc_empty + PL::kAccs);
     volatile int *abort_flag = reinterpret_cast<volatile int *>(tmem_slot + 1);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -206,8 +209,7 @@ __device__ __forceinline__ void act8_tn_body(const CUtensorMap &map_a, const CUt
 
     // full, acc_empty: of the pair's leader (rank 0), whose MMA warp waits on them; the others: each CTA's own
     if (threadIdx.x == 0) {
-        for (int s = 0; s < PL::kStages; ++s) { mbar_init(&full[s], 1 + kCtas * kDecodeWarps); mbar_init(&empty[s], 1); }
-        for (int q = 0; q < kRaw; ++q) { mbar_init(&raw_full[q], 1 + kScaleWarps); mbar_init(&raw_empty[q], kDecodeWarps); }
+        for (int s = 0; s < PL::kStages; ++s) { mbar_init(&full[s], 1 + kCtas * kGroupWarps); mbar_init(&empty[s], 1); mbar_init(&raw_full[s], 1 + kScaleWarps); mbar_init(&raw_empty[s], kGroupWarps); }
         for (int a = 0; a < PL::kAccs; ++a) { mbar_init(&acc_full[a], 1); mbar_init(&acc_empty[a], kCtas * kEpiWarps); }
         *abort_flag = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -302,7 +304,6 @@ __device__ __forceinline__ void act8_tn_body(const CUtensorMap &map_a, const CUt
         constexpr int kLead = 4;
         const bool one = warp == 2 && elect_one();
         const int r = (warp - 2) * 32 + lane;
-        int slot = 0;
         if (!g_skip_loads)
             for (int j = 0; ok && part_at(P, worker, j, part); ++j) {
                 const int col = (part.tile % P.tiles_k) * PL::kCols + (int)rank * kTileK, blocks = (P.No - col + kActBlock - 1) / kActBlock;
@@ -320,31 +321,33 @@ __device__ __forceinline__ void act8_tn_body(const CUtensorMap &map_a, const CUt
 #pragma unroll
                     for (int d = 0; d < kLead; ++d) {
                         if (i0 + d >= part.n) break;
-                        if (!(ok = warp_wait(smem_u32(&raw_empty[slot]), phase ^ 1u, abort_flag))) break;
+                        if (!(ok = warp_wait(smem_u32(&raw_empty[stage]), phase ^ 1u, abort_flag))) break;
                         if (one) {
-                            mbar_arrive_expect_tx(&raw_full[slot], kRawBytes);
-                            tma_load_2d(raw + (size_t)slot * kRawBytes, &map_h, &raw_full[slot], col, (part.k0 + i0 + d) * kBlockRows);
+                            mbar_arrive_expect_tx(&raw_full[stage], kRawBytes);
+                            tma_load_2d(raw + (size_t)stage * kRawBytes, &map_h, &raw_full[stage], col, (part.k0 + i0 + d) * kBlockRows);
                         }
-                        reinterpret_cast<uint32_t *>(scales + (size_t)slot * kScaleBytes)[r] = w[d];
+                        reinterpret_cast<uint32_t *>(scales + (size_t)stage * kScaleBytes)[r] = w[d];
                         __syncwarp();
-                        if (lane == 0) mbar_arrive(&raw_full[slot]);
+                        if (lane == 0) mbar_arrive(&raw_full[stage]);
                         ask(w[d]);
-                        if (++slot == kRaw) { slot = 0; phase ^= 1u; }
+                        if (++stage == PL::kStages) { stage = 0; phase ^= 1u; }
                     }
                 }
             }
     } else if (warp < kFirstEpi) {
-        // thread: 8 neighbouring columns of rows r and r + 32 of every k-block.  Eight lanes cover the 64 columns of a swizzled block
+        // Two groups of warps take the k-blocks in turn: the latencies of one's barriers, loads and fence lie under the other's work.
+        // thread: 8 neighbouring columns of rows r, r + 16, r + 32 and r + 48.  Eight lanes cover the 64 columns of a swizzled block
         // row, so that a 16-byte store phase meets all banks; the four rows of a warp are b, b + 4, b + 1, b + 5, so that the two
         // rows of a half warp lie in different halves of the codes' swizzle.
-        const int tid = (warp - kFirstDecode) * 32 + lane, half = tid >> 8, cq = tid & 7, w8 = (tid >> 5) & 7, l4 = (tid >> 3) & 3;
-        const int r = (w8 >> 1) * 8 + (w8 & 1) * 2 + (l4 & 1) * 4 + (l4 >> 1);
+        const int group = (warp - kFirstDecode) / kGroupWarps, w8 = (warp - kFirstDecode) % kGroupWarps;
+        const int half = w8 >> 2, cq = lane & 7, l4 = lane >> 3;
+        const int r = ((w8 >> 1) & 1) * 8 + (w8 & 1) * 2 + (l4 & 1) * 4 + (l4 >> 1);
         const uint32_t tile0 = smem_u32(tiles) + (uint32_t)(half * 8192 + r * 128) + (uint32_t)((cq ^ (r & 7)) << 4);
         const uint32_t raw0 = smem_u32(raw) + (uint32_t)(r * 128) + (uint32_t)(((half * 4 + (cq >> 1)) ^ (r & 7)) << 4) + (uint32_t)((cq & 1) * 8);
         const uint32_t scale0 = smem_u32(scales) + (uint32_t)(r * 4 + half * 2 + (cq >> 2));
-        const uint32_t full0 = PAIR ? map_to_rank(smem_u32(full), 0) : smem_u32(full);
-        int slot = 0;
-        uint32_t raw_phase = 0;
+        const uint32_t full0 = PAIR ? map_to_rank(smem_u32(full), 0) : smem_u32(full), raw_full0 = smem_u32(raw_full), raw_empty0 = smem_u32(raw_empty), empty0 = smem_u32(empty);
+        int taken = 0;
+        stage = group;
         for (int j = 0; ok && part_at(P, worker, j, part); ++j) {
             const int col = (part.tile % P.tiles_k) * PL::kCols + (int)rank * kTileK + half * 64 + cq * 8;
             F2 ga[MODE ? 4 : 1], be[MODE ? 4 : 1];
@@ -356,38 +359,39 @@ __device__ __forceinline__ void act8_tn_body(const CUtensorMap &map_a, const CUt
                     be[c] = f2(at_col(P.beta, col + 2 * c, 0.0f), at_col(P.beta, col + 2 * c + 1, 0.0f));
                 }
             }
-            int rows_left = P.R - part.k0 * kBlockRows;         // from this k-block on
-            for (int i = 0; i < part.n; ++i, rows_left -= kBlockRows) {
-                if (!(ok = warp_wait(smem_u32(&raw_full[slot]), raw_phase, abort_flag))) break;
-                uint2 w[2];
-                uint32_t byte[2];
+            // (taken: k-blocks of earlier parts; stage and phase: of this group's next one)
+            for (int i = (taken + group) & 1; i < part.n; i += 2) {
+                if (!(ok = warp_wait(raw_full0 + (uint32_t)(stage * 8), phase, abort_flag))) break;
+                const uint32_t from = raw0 + (uint32_t)(stage * kRawBytes), from_scale = scale0 + (uint32_t)(stage * kScaleBytes);
+                uint2 w[4];
+                uint32_t byte[4];
 #pragma unroll
-                for (int q = 0; q < 2; ++q) {
-                    asm volatile("ld.shared.v2.b32 {%0, %1}, [%2];" : "=r"(w[q].x), "=r"(w[q].y) : "r"(raw0 + (uint32_t)(slot * kRawBytes + q * 4096)) : "memory");
-                    asm volatile("ld.shared.u8 %0, [%1];" : "=r"(byte[q]) : "r"(scale0 + (uint32_t)(slot * kScaleBytes + q * 128)) : "memory");
+                for (int q = 0; q < 4; ++q) {
+                    asm volatile("ld.shared.v2.b32 {%0, %1}, [%2];" : "=r"(w[q].x), "=r"(w[q].y) : "r"(from + q * 2048) : "memory");
+                    asm volatile("ld.shared.u8 %0, [%1];" : "=r"(byte[q]) : "r"(from_scale + q * 64) : "memory");
                 }
-                uint32_t o[2][4];
+                if (!(ok = warp_wait(empty0 + (uint32_t)(stage * 8), phase ^ 1u, abort_flag))) break;
+                const uint32_t to = tile0 + (uint32_t)(stage * PL::kStageBytes);
+                const int rows_left = P.R - (part.k0 + i) * kBlockRows;
 #pragma unroll
-                for (int q = 0; q < 2; ++q) {
+                for (int q = 0; q < 4; ++q) {
+                    uint32_t o[4];
                     // (a marked block's byte, 255, is an infinity here, and its codes are 0: NaN)
-                    restore8<FORM, MODE>(w[q], __uint_as_float(byte[q] << 23), ga, be, o[q]);
-                    if (MODE && rows_left < kBlockRows && r + 32 * q >= rows_left) o[q][0] = o[q][1] = o[q][2] = o[q][3] = 0u;   // behind the last row: zeros, not beta
+                    restore8<FORM, MODE>(w[q], __uint_as_float(byte[q] << 23), ga, be, o);
+                    if (MODE && rows_left < kBlockRows && r + 16 * q >= rows_left) o[0] = o[1] = o[2] = o[3] = 0u;   // behind the last row: zeros, not beta
+                    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(to + q * 2048), "r"(o[0]), "r"(o[1]), "r"(o[2]), "r"(o[3]) : "memory");
                 }
-                if (!(ok = warp_wait(smem_u32(&empty[stage]), phase ^ 1u, abort_flag))) break;
-#pragma unroll
-                for (int q = 0; q < 2; ++q)
-                    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(tile0 + (uint32_t)(stage * PL::kStageBytes + q * 4096)), "r"(o[q][0]), "r"(o[q][1]),
-                                 "r"(o[q][2]), "r"(o[q][3]) : "memory");
                 asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                 __syncwarp();
                 if (lane == 0) {
-                    mbar_arrive(&raw_empty[slot]);
+                    mbar_arrive_addr(raw_empty0 + (uint32_t)(stage * 8));
                     if (PAIR) mbar_arrive_remote(full0 + (uint32_t)(stage * 8));
                     else mbar_arrive_addr(full0 + (uint32_t)(stage * 8));
                 }
-                if (++stage == PL::kStages) { stage = 0; phase ^= 1u; }
-                if (++slot == kRaw) { slot = 0; raw_phase ^= 1u; }
+                stage += 2;
+                if (stage >= PL::kStages) { stage -= PL::kStages; phase ^= 1u; }
             }
+            taken += part.n;
         }
     } else {
         // two warps per quadrant of tensor memory (lanes 32 quad .. 32 quad + 31), each with one half of the tile's columns
@@ -403,22 +407,26 @@ __device__ __forceinline__ void act8_tn_body(const CUtensorMap &map_a, const CUt
                 if (!(ok = warp_wait(smem_u32(&acc_full[acc]), acc_phase, abort_flag))) break;
                 tc_fence_after();
                 const uint32_t t_quad = tmem_base + ((uint32_t)(quad * 32) << 16), t_row = t_quad + (uint32_t)(acc * BLOCK_N), t_sum = t_quad + (uint32_t)(PL::kAccs * BLOCK_N);
-                // 16 columns at a time: the accumulator plus the sum so far, back into the sum, or out if it is the last chain
+                // 32 columns at a time: the accumulator plus the sum so far, back into the sum, or out if it is the last chain
                 const bool first = i0 == 0, last = i0 + kChainBlocks >= part.n;
-#pragma unroll 2
-                for (int c0 = c_first; c0 < c_first + BLOCK_N / 2; c0 += 16) {
-                    float v[16], sum[16];
-                    tmem_ld16_issue(t_row + (uint32_t)c0, v);
-                    if (!first) tmem_ld16_issue(t_sum + (uint32_t)c0, sum);
-                    tmem_ld_wait();
+#pragma unroll 1
+                for (int c0 = c_first; c0 < c_first + BLOCK_N / 2; c0 += 32) {
+                    float v[32];
+                    tmem_ld32_issue(t_row + (uint32_t)c0, v);
                     if (!first) {
 #pragma unroll
-                        for (int c = 0; c < 16; ++c) v[c] += sum[c];
-                    }
-                    if (!last) tmem_st16(t_sum + (uint32_t)c0, v);
+                        for (int h = 0; h < 32; h += 16) {
+                            float sum[16];
+                            tmem_ld16_issue(t_sum + (uint32_t)(c0 + h), sum);
+                            tmem_ld_wait();
+#pragma unroll
+                            for (int c = 0; c < 16; ++c) v[h + c] += sum[c];
+                        }
+                    } else tmem_ld_wait();
+                    if (!last) tmem_st32(t_sum + (uint32_t)c0, v);
                     else {
 #pragma unroll
-                        for (int c = 0; c < 16; ++c)
+                        for (int c = 0; c < 32; ++c)
                             if (c0 + c < rows) dst[(long long)(c0 + c) * ld] = v[c];
                     }
                 }
