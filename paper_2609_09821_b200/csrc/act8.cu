@@ -28,22 +28,9 @@ __global__ void __launch_bounds__(kThreads) pack_kernel(const T *x, long long ld
 #pragma unroll
         for (int i = 0; i < kRowsAtOnce; ++i) {
             const long long r = r0 + ty + i * row_step;
-            float v[8];
+            F2 v[4];
             unpack8(raw[i], v);
-            uint32_t amax = 0u;
-#pragma unroll
-            for (int j = 0; j < 8; ++j) amax = max(amax, abs_bits(v[j]));
-            amax = max(amax, __shfl_xor_sync(0xffffffffu, amax, 1));
-            amax = max(amax, __shfl_xor_sync(0xffffffffu, amax, 2));
-            const uint32_t byte = act8_scale_byte(amax, out.form);
-            const float inv = byte == 255u ? 0.0f : act8_inverse(byte);
-#pragma unroll
-            for (int j = 0; j < 8; ++j) v[j] = byte == 255u ? 0.0f : v[j] * inv;
-            if (r < M && col < N) {
-                store_codes8<VEC>(out.code + r * out.ld_code, col, 1, N,
-                                  make_uint2(act8_encode4(v[0], v[1], v[2], v[3], out.form), act8_encode4(v[4], v[5], v[6], v[7], out.form)));
-                if ((tx & 3) == 0) out.scale[r * out.ld_scale + (col >> 5)] = (uint8_t)byte;
-            }
+            keep8<true, VEC, 1>(out, r < M, r, col, N, v);
         }
     }
 }
@@ -55,12 +42,13 @@ __global__ void __launch_bounds__(kThreads) unpack_kernel(const Act8View in, int
     const int tx = threadIdx.x & ((1 << tx_bits) - 1), ty = threadIdx.x >> tx_bits, rows_per_cta = kThreads >> tx_bits;
     const int col = (((int)blockIdx.x << tx_bits) + tx) * 8;
     const long long row_step = (long long)gridDim.y * rows_per_cta;
-    float g[8], b[8];
+    F2 g[4], b[4];
     if (AFFINE) {
+        const auto at = [&](const float *p, int k, float other) { return p && k < N ? __ldg(p + k) : other; };
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            g[j] = gamma && col + j < N ? __ldg(gamma + col + j) : 1.0f;
-            b[j] = beta && col + j < N ? __ldg(beta + col + j) : 0.0f;
+        for (int j = 0; j < 4; ++j) {
+            g[j] = f2(at(gamma, col + 2 * j, 1.0f), at(gamma, col + 2 * j + 1, 1.0f));
+            b[j] = f2(at(beta, col + 2 * j, 0.0f), at(beta, col + 2 * j + 1, 0.0f));
         }
     }
     if (col >= N) return;
@@ -77,19 +65,14 @@ __global__ void __launch_bounds__(kThreads) unpack_kernel(const Act8View in, int
         for (int i = 0; i < kRowsAtOnce; ++i) {
             const long long r = r0 + i * row_step;
             if (r >= M) break;
-            float v[8];
-            act8_decode4(raw[i].x, in.form, *reinterpret_cast<float(*)[4]>(v));
-            act8_decode4(raw[i].y, in.form, *reinterpret_cast<float(*)[4]>(v + 4));
-            const float s = act8_scale(byte[i]);
+            F2 v[4];
+            act8_restore8(raw[i], byte[i], in.form, v);
+            if (AFFINE) {
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                v[j] *= s;
-                if (AFFINE) {
-                    v[j] = __fmaf_rn(g[j], v[j], b[j]);
-                    if (relu) v[j] = v[j] < 0.0f ? 0.0f : v[j];         // (a NaN stays)
-                }
+                for (int j = 0; j < 4; ++j) v[j] = fma2(g[j], v[j], b[j]);
             }
-            store8<VEC>(out + r * ld_out, col, 1, N, v);
+            if (AFFINE && relu) store8<VEC, true>(out + r * ld_out, col, 1, N, v);
+            else store8<VEC, false>(out + r * ld_out, col, 1, N, v);
         }
     }
 }

@@ -124,12 +124,19 @@ __device__ __forceinline__ void act8_decode4(uint32_t w, F2 &a, F2 &b)
     a = f2(v[0], v[1]);
     b = f2(v[2], v[3]);
 }
-__device__ __forceinline__ void act8_decode4(uint32_t w, int form, float (&v)[4])
+// Eight values, with their scale.
+__device__ __forceinline__ void act8_restore8(const uint2 &w, uint32_t byte, int form, F2 *v)
 {
-    F2 a, b;
-    if (form == IM_ACT8_INT8) act8_decode4<IM_ACT8_INT8>(w, a, b);
-    else act8_decode4<IM_ACT8_E4M3>(w, a, b);
-    v[0] = lo(a); v[1] = hi(a); v[2] = lo(b); v[3] = hi(b);
+    if (form == IM_ACT8_INT8) {
+        act8_decode4<IM_ACT8_INT8>(w.x, v[0], v[1]);
+        act8_decode4<IM_ACT8_INT8>(w.y, v[2], v[3]);
+    } else {
+        act8_decode4<IM_ACT8_E4M3>(w.x, v[0], v[1]);
+        act8_decode4<IM_ACT8_E4M3>(w.y, v[2], v[3]);
+    }
+    const F2 s = f2(act8_scale(byte));
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] = mul2(v[i], s);
 }
 
 // ------------------------------------------------------------------ rows of fp32 or bf16 values
@@ -167,46 +174,44 @@ __device__ __forceinline__ Eight<T> load8(const T *row, int col, int step, int c
     }
     return e;
 }
-__device__ __forceinline__ void unpack8(const Eight<float> &e, float *v)
+__device__ __forceinline__ void unpack8(const Eight<float> &e, F2 *v)
 {
-    v[0] = e.a.x; v[1] = e.a.y; v[2] = e.a.z; v[3] = e.a.w;
-    v[4] = e.b.x; v[5] = e.b.y; v[6] = e.b.z; v[7] = e.b.w;
+    v[0] = f2(e.a.x, e.a.y); v[1] = f2(e.a.z, e.a.w);
+    v[2] = f2(e.b.x, e.b.y); v[3] = f2(e.b.z, e.b.w);
 }
-__device__ __forceinline__ void unpack8(const Eight<__nv_bfloat16> &e, float *v)
+__device__ __forceinline__ void unpack8(const Eight<__nv_bfloat16> &e, F2 *v)
 {
     const uint32_t w[4] = {e.a.x, e.a.y, e.a.z, e.a.w};
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        v[2 * i] = __uint_as_float(w[i] << 16);
-        v[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
-    }
+    for (int i = 0; i < 4; ++i) v[i] = f2(__uint_as_float(w[i] << 16), __uint_as_float(w[i] & 0xffff0000u));
 }
-__device__ __forceinline__ void full_store8(float *p, const float *v)
+// RELU: negative values become 0, a NaN stays one.
+template <bool RELU>
+__device__ __forceinline__ float floored(float x) { return RELU && x < 0.0f ? 0.0f : x; }
+template <bool RELU>
+__device__ __forceinline__ void full_store8(float *p, const F2 *v)
 {
-    reinterpret_cast<float4 *>(p)[0] = make_float4(v[0], v[1], v[2], v[3]);
-    reinterpret_cast<float4 *>(p)[1] = make_float4(v[4], v[5], v[6], v[7]);
+    float4 a = make_float4(floored<RELU>(lo(v[0])), floored<RELU>(hi(v[0])), floored<RELU>(lo(v[1])), floored<RELU>(hi(v[1])));
+    float4 b = make_float4(floored<RELU>(lo(v[2])), floored<RELU>(hi(v[2])), floored<RELU>(lo(v[3])), floored<RELU>(hi(v[3])));
+    reinterpret_cast<float4 *>(p)[0] = a;
+    reinterpret_cast<float4 *>(p)[1] = b;
 }
-__device__ __forceinline__ void full_store8(__nv_bfloat16 *p, const float *v)
+template <bool RELU>
+__device__ __forceinline__ void full_store8(__nv_bfloat16 *p, const F2 *v)
 {
-    uint32_t w[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const __nv_bfloat162 h = __floats2bfloat162_rn(v[2 * i], v[2 * i + 1]);
-        w[i] = *reinterpret_cast<const uint32_t *>(&h);
-    }
-    *reinterpret_cast<uint4 *>(p) = make_uint4(w[0], w[1], w[2], w[3]);
+    *reinterpret_cast<uint4 *>(p) = make_uint4(bf16x2<RELU>(v[0]), bf16x2<RELU>(v[1]), bf16x2<RELU>(v[2]), bf16x2<RELU>(v[3]));
 }
-template <bool VEC, typename T>
-__device__ __forceinline__ void store8(T *row, int col, int step, int cols, const float *v)
+template <bool VEC, bool RELU, typename T>
+__device__ __forceinline__ void store8(T *row, int col, int step, int cols, const F2 *v)
 {
     if (VEC && col + 8 <= cols) {
-        full_store8(row + col, v);
+        full_store8<RELU>(row + col, v);
         return;
     }
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
         const int c = VEC ? col + j : col + j * step;
-        if (c < cols) store_as(row + c, v[j]);
+        if (c < cols) store_as(row + c, floored<RELU>(j & 1 ? hi(v[j >> 1]) : lo(v[j >> 1])));
     }
 }
 // Eight codes of a row, in the same two arrangements.
@@ -234,6 +239,44 @@ __device__ __forceinline__ void store_codes8(uint8_t *row, int col, int step, in
         const int c = VEC ? col + j : col + j * step;
         if (c < cols) row[c] = (uint8_t)((j < 4 ? w.x : w.y) >> (8 * (j & 3)));
     }
+}
+
+// Scale byte and codes of a thread's eight values of a row.  SIDE: they are neighbours, and four threads in a row make a block; else
+// they lie T columns apart, and a block is one value of each lane.  ALIGNED: eight codes may be stored at once (SIDE only).
+// Whole warps; in: the row exists.
+template <bool SIDE, bool ALIGNED, int T>
+__device__ __forceinline__ void keep8(const Act8View &k, bool in, long long row, int col, int cols, const F2 *v)
+{
+    const auto at = [&](int j) { return j & 1 ? hi(v[j >> 1]) : lo(v[j >> 1]); };
+    float q[8];
+    if (SIDE) {
+        uint32_t amax = 0u;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) amax = max(amax, col + j < cols ? abs_bits(at(j)) : 0u);
+        amax = max(amax, __shfl_xor_sync(0xffffffffu, amax, 1));
+        amax = max(amax, __shfl_xor_sync(0xffffffffu, amax, 2));
+        const uint32_t byte = act8_scale_byte(amax, k.form);
+        const F2 inv = f2(byte == 255u ? 0.0f : act8_inverse(byte));
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const F2 x = mul2(v[i], inv);
+            q[2 * i] = byte == 255u ? 0.0f : lo(x);
+            q[2 * i + 1] = byte == 255u ? 0.0f : hi(x);
+        }
+        if (!in || col >= cols) return;
+        if ((col & 31) == 0) k.scale[row * k.ld_scale + (col >> 5)] = (uint8_t)byte;
+    } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const int c = col + j * T;
+            const uint32_t byte = act8_scale_byte(__reduce_max_sync(0xffffffffu, c < cols ? abs_bits(at(j)) : 0u), k.form);
+            q[j] = byte == 255u ? 0.0f : at(j) * act8_inverse(byte);
+            if (in && (c & 31) == 0 && c < cols) k.scale[row * k.ld_scale + (c >> 5)] = (uint8_t)byte;
+        }
+        if (!in) return;
+    }
+    store_codes8<SIDE && ALIGNED>(k.code + row * k.ld_code, col, SIDE ? 1 : T, cols,
+                                  make_uint2(act8_encode4(q[0], q[1], q[2], q[3], k.form), act8_encode4(q[4], q[5], q[6], q[7], k.form)));
 }
 
 inline bool aligned_to(const void *p, uintptr_t bytes) { return (reinterpret_cast<uintptr_t>(p) & (bytes - 1)) == 0; }

@@ -32,17 +32,28 @@ __device__ __forceinline__ float row_sum(float v, float *shared)
 }
 
 // T threads share a row, each holding C groups of eight values: VEC neighbours, else every T-th column.
+// gamma and beta lie in shared memory, in the order in which the threads read them (16 bytes a lane side by side): in registers
+// they would take twice the row's own share, and read from L1 anew for every row they cost 8 loads per group.
 template <typename TX, typename TY, bool VEC, int T, int C>
 __global__ void __launch_bounds__(kThreads) norm_forward_kernel(const NormForward P)
 {
     constexpr int kGroups = kThreads / T;                         // rows of a CTA at a time
     __shared__ float s_sum[2][kThreads / 32];
+    extern __shared__ float4 s_affine[];                          // [gamma, beta][C][2][T]
     const int t = threadIdx.x & (T - 1), g = threadIdx.x / T, N = P.N;
     const TX *x = static_cast<const TX *>(P.x);
     TY *y = static_cast<TY *>(P.y);
     const auto first = [&](int c) { return VEC ? (c * T + t) * 8 : c * 8 * T + t; };
+    constexpr int kStep = VEC ? 1 : T;                            // between a group's columns
     const float n = (float)N;
 
+    for (int i = threadIdx.x; i < 8 * C * T; i += kThreads) {
+        // element i of the layout: group c, half h, thread tt, position p of four
+        const int p = i & 3, tt = (i >> 2) & (T - 1), h = (i >> 2) / T & 1, c = (i >> 2) / (2 * T);
+        const int col = VEC ? (c * T + tt) * 8 + h * 4 + p : c * 8 * T + (h * 4 + p) * T + tt;
+        reinterpret_cast<float *>(s_affine)[i] = P.gamma && col < N ? __ldg(P.gamma + col) : 1.0f;
+        reinterpret_cast<float *>(s_affine)[8 * C * T + i] = P.beta && col < N ? __ldg(P.beta + col) : 0.0f;
+    }
     Eight<TX> raw[C];
     const auto load_row = [&](long long r) {
 #pragma unroll
@@ -50,78 +61,54 @@ __global__ void __launch_bounds__(kThreads) norm_forward_kernel(const NormForwar
     };
     const long long step = (long long)gridDim.x * kGroups;
     load_row((long long)blockIdx.x * kGroups + g);
+    __syncthreads();
     for (long long base = (long long)blockIdx.x * kGroups; base < P.M; base += step) {       // (the whole CTA together)
         const long long r = base + g;
-        float v[8 * C];
+        F2 v[4 * C];
 #pragma unroll
-        for (int c = 0; c < C; ++c) unpack8(raw[c], v + 8 * c);
+        for (int c = 0; c < C; ++c) unpack8(raw[c], v + 4 * c);
         if (base + step < P.M) load_row(r + step);
-        float s = 0.0f;
+        F2 s = v[0];
 #pragma unroll
-        for (int i = 0; i < 8 * C; ++i) s += v[i];
-        const float mean = row_sum<T>(s, s_sum[0]) / n;
-        s = 0.0f;
+        for (int i = 1; i < 4 * C; ++i) s = add2(s, v[i]);
+        const float mean = row_sum<T>(lo(s) + hi(s), s_sum[0]) / n;
+        const F2 minus = f2(-mean);
+        s = f2(0.0f);
 #pragma unroll
-        for (int c = 0; c < C; ++c)
+        for (int c = 0; c < C; ++c) {
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                const float d = __fsub_rn(v[8 * c + j], mean);
-                v[8 * c + j] = d;
-                if (VEC ? first(c) + j < N : first(c) + j * T < N) s = fmaf(d, d, s);
+            for (int i = 0; i < 4; ++i) v[4 * c + i] = add2(v[4 * c + i], minus);
+            if (first(c) + 7 * kStep >= N) {                       // columns behind the last
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    v[4 * c + i] = f2(first(c) + 2 * i * kStep < N ? lo(v[4 * c + i]) : 0.0f, first(c) + (2 * i + 1) * kStep < N ? hi(v[4 * c + i]) : 0.0f);
             }
-        const float rstd = 1.0f / sqrtf(row_sum<T>(s, s_sum[1]) / n + P.eps);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) s = fma2(v[4 * c + i], v[4 * c + i], s);
+        }
+        const float rstd = 1.0f / sqrtf(row_sum<T>(lo(s) + hi(s), s_sum[1]) / n + P.eps);
         if (r < P.M && t == 0) {
             if (P.mean) P.mean[r] = mean;
             if (P.rstd) P.rstd[r] = rstd;
         }
+        const F2 scale = f2(rstd);
 #pragma unroll
         for (int c = 0; c < C; ++c) {
             const int col = first(c);
-            float *e = v + 8 * c;
+            F2 *e = v + 4 * c;
 #pragma unroll
-            for (int j = 0; j < 8; ++j) e[j] = __fmul_rn(e[j], rstd);     // xh, by the operations that the backward pass repeats
-            if (P.keep.code) {
-                const auto in_row = [&](int j) { return VEC ? col + j < N : col + j * T < N; };
-                if (VEC) {
-                    uint32_t amax = 0u;
+            for (int i = 0; i < 4; ++i) e[i] = mul2(e[i], scale);      // xh, by the operations that the backward pass repeats
+            if (P.keep.code) keep8<VEC, VEC, T>(P.keep, r < P.M, r, col, N, e);
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) amax = max(amax, in_row(j) ? abs_bits(e[j]) : 0u);
-                    amax = max(amax, __shfl_xor_sync(0xffffffffu, amax, 1));
-                    amax = max(amax, __shfl_xor_sync(0xffffffffu, amax, 2));
-                    const uint32_t byte = act8_scale_byte(amax, P.keep.form);
-                    const float inv = byte == 255u ? 0.0f : act8_inverse(byte);
-                    float q[8];
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) q[j] = byte == 255u ? 0.0f : e[j] * inv;
-                    if (r < P.M && col < N) {
-                        store_codes8<true>(P.keep.code + r * P.keep.ld_code, col, T, N,
-                                           make_uint2(act8_encode4(q[0], q[1], q[2], q[3], P.keep.form), act8_encode4(q[4], q[5], q[6], q[7], P.keep.form)));
-                        if ((t & 3) == 0) P.keep.scale[r * P.keep.ld_scale + (col >> 5)] = (uint8_t)byte;
-                    }
-                } else {
-                    // the 32 columns of a block are a warp's 32 lanes at one j
-                    uint32_t w[2] = {0u, 0u};
-                    float q[8];
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) {
-                        const uint32_t amax = __reduce_max_sync(0xffffffffu, in_row(j) ? abs_bits(e[j]) : 0u);
-                        const uint32_t byte = act8_scale_byte(amax, P.keep.form);
-                        q[j] = byte == 255u ? 0.0f : e[j] * act8_inverse(byte);
-                        if ((threadIdx.x & 31) == 0 && r < P.M && in_row(j)) P.keep.scale[r * P.keep.ld_scale + ((col + j * T) >> 5)] = (uint8_t)byte;
-                    }
-                    w[0] = act8_encode4(q[0], q[1], q[2], q[3], P.keep.form);
-                    w[1] = act8_encode4(q[4], q[5], q[6], q[7], P.keep.form);
-                    if (r < P.M) store_codes8<false>(P.keep.code + r * P.keep.ld_code, col, T, N, make_uint2(w[0], w[1]));
-                }
+            for (int h = 0; h < 2; ++h) {
+                const float4 ga = s_affine[(2 * c + h) * T + t], be = s_affine[(2 * (C + c) + h) * T + t];
+                e[2 * h] = fma2(f2(ga.x, ga.y), e[2 * h], f2(be.x, be.y));
+                e[2 * h + 1] = fma2(f2(ga.z, ga.w), e[2 * h + 1], f2(be.z, be.w));
             }
-#pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                const int k = VEC ? col + j : col + j * T;
-                const float ga = P.gamma && k < N ? __ldg(P.gamma + k) : 1.0f, be = P.beta && k < N ? __ldg(P.beta + k) : 0.0f;
-                e[j] = __fmaf_rn(ga, e[j], be);
-                if (P.relu) e[j] = e[j] < 0.0f ? 0.0f : e[j];              // (a NaN stays)
+            if (r < P.M) {
+                if (P.relu) store8<VEC, true>(y + r * P.ldy, col, T, N, e);
+                else store8<VEC, false>(y + r * P.ldy, col, T, N, e);
             }
-            if (r < P.M) store8<VEC>(y + r * P.ldy, col, T, N, e);
         }
     }
 }
@@ -150,8 +137,22 @@ template <typename TX, typename TY, bool VEC, int T, int C>
 cudaError_t launch_forward(const NormForward &a, int n_sm, cudaStream_t stream)
 {
     constexpr int kGroups = kThreads / T;
-    const long long want = ((long long)a.M + kGroups - 1) / kGroups, most = (long long)n_sm * 8;
-    norm_forward_kernel<TX, TY, VEC, T, C><<<(unsigned)(want < most ? want : most), kThreads, 0, stream>>>(a);
+    constexpr size_t kSmem = (size_t)2 * 8 * C * T * sizeof(float);
+    const auto kernel = norm_forward_kernel<TX, TY, VEC, T, C>;
+    static DeviceOnce once;
+    static std::atomic<int> per_sm[kMaxDevices];                  // CTAs that fit an SM
+    int dev = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e == cudaSuccess) e = once.run([&] {
+        cudaError_t r = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSmem);
+        int fit = 0;
+        if (r == cudaSuccess) r = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&fit, kernel, kThreads, kSmem);
+        per_sm[dev].store(fit < 1 ? 1 : fit);
+        return r;
+    });
+    if (e != cudaSuccess) return e;
+    const long long want = ((long long)a.M + kGroups - 1) / kGroups, most = (long long)n_sm * per_sm[dev].load();
+    kernel<<<(unsigned)(want < most ? want : most), kThreads, kSmem, stream>>>(a);
     return cudaGetLastError();
 }
 template <typename TX, typename TY>

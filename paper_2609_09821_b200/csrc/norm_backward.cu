@@ -7,7 +7,7 @@
 // normalised to, so the ReLU opens the same elements; or from an 8-bit checkpoint of it.
 // A thread owns eight columns for the whole launch: their share of dgamma and dbeta stays in registers over all rows that
 // the CTA walks, and is written once, as one row of partial sums per CTA (summed in fp64 in a fixed order by a second
-// kernel, so results are bit-reproducible).  The two row means are sums over the 8 to 1024 threads of a row.
+// kernel, so results are bit-reproducible).  The two row means are sums over the 8 to 512 threads of a row.
 // What bounds it is HBM: x (or its codes) and dy are read once, dx is written once.
 #include "im_internal.h"
 #include "norm.h"
@@ -18,161 +18,219 @@ namespace {
 
 constexpr __host__ __device__ int cta_threads(int T) { return T > 256 ? T : 256; }
 
-template <typename TX, typename TY, bool VEC, int T, int R, bool KEPT>
-__global__ void __launch_bounds__(cta_threads(T)) norm_backward_kernel(const NormBackward P)
+// The sums of K values (a power of two, at most 4) over the T lanes of a row, or over a warp if T is more; in every lane.
+template <int T, int K>
+__device__ __forceinline__ void lane_sums(float (&s)[K])
 {
-    constexpr int kCta = cta_threads(T), kGroups = kCta / T;
+    constexpr unsigned kAll = 0xffffffffu;
+    if (T < 32 || K == 1) {
+#pragma unroll
+        for (int k = 0; k < K; ++k)
+#pragma unroll
+            for (int o = (T < 32 ? T : 32) / 2; o > 0; o >>= 1) s[k] += __shfl_xor_sync(kAll, s[k], o);
+        return;
+    }
+    // each half of the lanes goes on with one half of the values: K - 1 + (5 - log2 K) + K exchanges for K x 5
+    const int lane = threadIdx.x & 31;
+    float a[2], one;
+    if (K == 4) {
+        const bool up = lane & 16;
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            const float keep = up ? s[2 + k] : s[k], send = up ? s[k] : s[2 + k];
+            a[k] = keep + __shfl_xor_sync(kAll, send, 16);
+        }
+    } else { a[0] = s[0]; a[1] = s[K - 1]; }
+    constexpr int o2 = K == 4 ? 8 : 16;
+    const bool up = lane & o2;
+    one = (up ? a[1] : a[0]) + __shfl_xor_sync(kAll, up ? a[0] : a[1], o2);
+#pragma unroll
+    for (int o = o2 / 2; o > 0; o >>= 1) one += __shfl_xor_sync(kAll, one, o);
+#pragma unroll
+    for (int k = 0; k < K; ++k) s[k] = __shfl_sync(kAll, one, K == 4 ? (k >> 1) * 16 + (k & 1) * 8 : k * 16);
+}
+
+// T threads share a row; each owns C groups of eight columns: VEC neighbours, else every T-th.  A group of T threads takes R rows
+// at a time.
+template <typename TX, typename TY, bool VEC, int T, int C, int R, bool KEPT>
+__global__ void __launch_bounds__(cta_threads(T), 512 / cta_threads(T)) norm_backward_kernel(const NormBackward P)
+{
+    constexpr int kCta = cta_threads(T), kGroups = kCta / T, E = 4 * C;
     constexpr int kWarps = T / 32;                                       // of a row (0: less than one)
     __shared__ float s_red[2][kGroups][kWarps > 0 ? kWarps : 1][2 * R];
     __shared__ float s_col[kGroups > 1 ? kCta * 16 : 1];
     const int t = threadIdx.x & (T - 1), g = threadIdx.x / T, N = P.N;
-    const int col = VEC ? t * 8 : t;
+    const auto first = [&](int c) { return VEC ? (c * T + t) * 8 : c * 8 * T + t; };
+    constexpr int kStep = VEC ? 1 : T;
     const TX *x = static_cast<const TX *>(P.x);
     TX *dx = static_cast<TX *>(P.dx);
     const TY *dy = static_cast<const TY *>(P.dy);
-    float ga[8], be[8], acc_g[8], acc_b[8];
+    F2 ga[E], be[E], acc_g[E], acc_b[E];
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-        const int k = VEC ? col + j : col + j * T;
-        ga[j] = P.gamma && k < N ? __ldg(P.gamma + k) : (k < N ? 1.0f : 0.0f);
-        be[j] = P.beta && k < N ? __ldg(P.beta + k) : 0.0f;
-        acc_g[j] = acc_b[j] = 0.0f;
+    for (int i = 0; i < E; ++i) {
+        const int k = first(i >> 2) + 2 * (i & 3) * kStep;
+        const auto at = [&](const float *p, int c, float other) { return c >= N ? 0.0f : p ? __ldg(p + c) : other; };
+        ga[i] = f2(at(P.gamma, k, 1.0f), at(P.gamma, k + kStep, 1.0f));
+        be[i] = f2(at(P.beta, k, 0.0f), at(P.beta, k + kStep, 0.0f));
+        acc_g[i] = acc_b[i] = f2(0.0f);
     }
     const float inv_n = 1.0f / (float)N;
     int buf = 0;
-    const long long step = (long long)gridDim.x * kGroups * R;
-    for (long long base = (long long)blockIdx.x * kGroups * R; base < P.M; base += step) {     // (the whole CTA together)
-        Eight<TX> rx[R];
-        Eight<TY> ry[R];
-        uint2 code[R];
-        uint32_t byte[R];
+    // what a batch of rows needs from memory; columns behind the last are zeros there, and so are their shares of all sums
+    struct Batch {
+        Eight<TX> x[KEPT ? 1 : R][C];
+        Eight<TY> y[R][C];
+        uint2 code[KEPT ? R : 1][C];
+        uint32_t byte[KEPT && VEC ? R : 1][C];
         float mean[R], rstd[R];
+    } raw;
+    const auto load = [&](long long base) {
 #pragma unroll
         for (int i = 0; i < R; ++i) {
             const long long r = base + (long long)i * kGroups + g;
             const bool in = r < P.M;
-            ry[i] = in ? load8<VEC>(dy + r * P.ld_dy, col, T, N) : zero8(dy);
-            rstd[i] = in ? P.rstd[r] : 0.0f;
-            if (KEPT) {
-                code[i] = in ? load_codes8<VEC>(P.kept.code + r * P.kept.ld_code, col, T, N) : make_uint2(0u, 0u);
-                if (VEC) byte[i] = in && col < N ? P.kept.scale[r * P.kept.ld_scale + (col >> 5)] : 0u;
-            } else {
-                rx[i] = in ? load8<VEC>(x + r * P.ldx, col, T, N) : zero8(x);
-                mean[i] = in ? P.mean[r] : 0.0f;
+#pragma unroll
+            for (int c = 0; c < C; ++c) {
+                raw.y[i][c] = in ? load8<VEC>(dy + r * P.ld_dy, first(c), T, N) : zero8(dy);
+                if (KEPT) {
+                    raw.code[i][c] = in ? load_codes8<VEC>(P.kept.code + r * P.kept.ld_code, first(c), T, N) : make_uint2(0u, 0u);
+                    if (VEC) raw.byte[i][c] = in && first(c) < N ? P.kept.scale[r * P.kept.ld_scale + (first(c) >> 5)] : 0u;
+                } else raw.x[i][c] = in ? load8<VEC>(x + r * P.ldx, first(c), T, N) : zero8(x);
             }
+            raw.rstd[i] = in ? P.rstd[r] : 0.0f;
+            if (!KEPT) raw.mean[i] = in ? P.mean[r] : 0.0f;
         }
-        float xh[R][8], h[R][8], s[2 * R];
+    };
+    const long long step = (long long)gridDim.x * kGroups * R;
+    load((long long)blockIdx.x * kGroups * R);
+    for (long long base = (long long)blockIdx.x * kGroups * R; base < P.M; base += step) {     // (the whole CTA together)
+        F2 xh[R][E], h[R][E];
+        float s[2 * R], rstd[R];
 #pragma unroll
         for (int i = 0; i < R; ++i) {
-            const long long r = base + (long long)i * kGroups + g;
-            unpack8(ry[i], h[i]);
-            if (KEPT) {
-                act8_decode4(code[i].x, P.kept.form, *reinterpret_cast<float(*)[4]>(xh[i]));
-                act8_decode4(code[i].y, P.kept.form, *reinterpret_cast<float(*)[4]>(xh[i] + 4));
-                if (VEC) {
-                    const float sc = act8_scale(byte[i]);
+            rstd[i] = raw.rstd[i];
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) xh[i][j] = col + j < N ? xh[i][j] * sc : 0.0f;
+            for (int c = 0; c < C; ++c) {
+                unpack8(raw.y[i][c], h[i] + 4 * c);
+                if (!KEPT) {
+                    unpack8(raw.x[i][c], xh[i] + 4 * c);
+                    const F2 minus = f2(-raw.mean[i]), scale = f2(raw.rstd[i]);
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) xh[i][4 * c + j] = mul2(add2(xh[i][4 * c + j], minus), scale);
+                } else if (VEC) {
+                    act8_restore8(raw.code[i][c], raw.byte[i][c], P.kept.form, xh[i] + 4 * c);
                 } else {
+                    const long long r = base + (long long)i * kGroups + g;
+                    act8_restore8(raw.code[i][c], 127u, P.kept.form, xh[i] + 4 * c);
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) {
-                        const int k = col + j * T;
-                        xh[i][j] = r < P.M && k < N ? xh[i][j] * act8_scale(P.kept.scale[r * P.kept.ld_scale + (k >> 5)]) : 0.0f;
+                    for (int j = 0; j < 4; ++j) {
+                        const int k = first(c) + 2 * j * kStep;
+                        const auto scale = [&](int col) { return r < P.M && col < N ? act8_scale(P.kept.scale[r * P.kept.ld_scale + (col >> 5)]) : 0.0f; };
+                        xh[i][4 * c + j] = mul2(xh[i][4 * c + j], f2(scale(k), scale(k + kStep)));
                     }
                 }
-            } else {
-                unpack8(rx[i], xh[i]);
-#pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    const int k = VEC ? col + j : col + j * T;
-                    xh[i][j] = k < N ? __fmul_rn(__fsub_rn(xh[i][j], mean[i]), rstd[i]) : 0.0f;
-                }
             }
-            float s1 = 0.0f, s2 = 0.0f;
-#pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                if (P.relu && !(__fmaf_rn(ga[j], xh[i][j], be[j]) > 0.0f)) h[i][j] = 0.0f;
-                const float gh = ga[j] * h[i][j];
-                s1 += gh;
-                s2 = fmaf(gh, xh[i][j], s2);
-                acc_b[j] += h[i][j];
-                acc_g[j] = fmaf(h[i][j], xh[i][j], acc_g[j]);
-            }
-            s[2 * i] = s1;
-            s[2 * i + 1] = s2;
         }
+        if (base + step < P.M) load(base + step);
 #pragma unroll
-        for (int k = 0; k < 2 * R; ++k)
+        for (int i = 0; i < R; ++i) {
+            F2 s1 = f2(0.0f), s2 = f2(0.0f);
 #pragma unroll
-            for (int o = (T < 32 ? T : 32) / 2; o > 0; o >>= 1) s[k] += __shfl_xor_sync(0xffffffffu, s[k], o);
+            for (int e = 0; e < E; ++e) {
+                if (P.relu) {
+                    const F2 y = fma2(ga[e], xh[i][e], be[e]);
+                    h[i][e] = f2(lo(y) > 0.0f ? lo(h[i][e]) : 0.0f, hi(y) > 0.0f ? hi(h[i][e]) : 0.0f);
+                }
+                const F2 gh = mul2(ga[e], h[i][e]);
+                s1 = add2(s1, gh);
+                s2 = fma2(gh, xh[i][e], s2);
+                acc_b[e] = add2(acc_b[e], h[i][e]);
+                acc_g[e] = fma2(h[i][e], xh[i][e], acc_g[e]);
+            }
+            s[2 * i] = lo(s1) + hi(s1);
+            s[2 * i + 1] = lo(s2) + hi(s2);
+        }
+        lane_sums<T>(s);
         if (T > 32) {
             if ((threadIdx.x & 31) == 0) {
 #pragma unroll
                 for (int k = 0; k < 2 * R; ++k) s_red[buf][g][t >> 5][k] = s[k];
             }
-            __syncthreads();                    // (two buffers: nobody still reads the one that is written next)
+            // the row group's own barrier (two buffers: nobody still reads the one that is written next)
+            asm volatile("bar.sync %0, %1;" ::"r"(1 + g), "n"(T) : "memory");
 #pragma unroll
-            for (int k = 0; k < 2 * R; ++k) {
-                s[k] = 0.0f;
+            for (int k = 0; k < 2 * R; ++k) s[k] = 0.0f;
 #pragma unroll
-                for (int w = 0; w < kWarps; ++w) s[k] += s_red[buf][g][w][k];
-            }
+            for (int w = 0; w < kWarps; ++w)
+#pragma unroll
+                for (int k = 0; k < 2 * R; ++k) s[k] += s_red[buf][g][w][k];
             buf ^= 1;
         }
         if (dx) {
 #pragma unroll
             for (int i = 0; i < R; ++i) {
                 const long long r = base + (long long)i * kGroups + g;
-                const float c1 = s[2 * i] * inv_n, c2 = s[2 * i + 1] * inv_n;
-                float out[8];
+                const F2 minus_c1 = f2(-(s[2 * i] * inv_n)), minus_c2 = f2(-(s[2 * i + 1] * inv_n)), scale = f2(rstd[i]);
 #pragma unroll
-                for (int j = 0; j < 8; ++j) out[j] = rstd[i] * (fmaf(ga[j], h[i][j], -c1) - xh[i][j] * c2);
-                if (r < P.M) store8<VEC>(dx + r * P.ld_dx, col, T, N, out);
+                for (int c = 0; c < C; ++c) {
+                    F2 out[4];
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        const int e = 4 * c + j;
+                        out[j] = mul2(scale, fma2(xh[i][e], minus_c2, fma2(ga[e], h[i][e], minus_c1)));
+                    }
+                    if (r < P.M) store8<VEC, false>(dx + r * P.ld_dx, first(c), T, N, out);
+                }
             }
         }
     }
     if (!P.partial) return;
     float *row = P.partial + (long long)blockIdx.x * 2 * N;
     if (kGroups > 1) {
-        // one slot per column and kind: columns of a thread lie kCta / kGroups apart, so that lanes meet no bank twice
+        // one slot per column and kind; neighbouring threads' slots lie side by side
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            s_col[(j * 2 + 0) * kCta + g * T + t] = acc_g[j];
-            s_col[(j * 2 + 1) * kCta + g * T + t] = acc_b[j];
+        for (int e = 0; e < E; ++e) {
+            s_col[(4 * e + 0) * kCta + threadIdx.x] = lo(acc_g[e]);
+            s_col[(4 * e + 1) * kCta + threadIdx.x] = hi(acc_g[e]);
+            s_col[(4 * e + 2) * kCta + threadIdx.x] = lo(acc_b[e]);
+            s_col[(4 * e + 3) * kCta + threadIdx.x] = hi(acc_b[e]);
         }
         __syncthreads();
         if (g == 0) {
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                acc_g[j] = acc_b[j] = 0.0f;
+            for (int e = 0; e < E; ++e) {
+                acc_g[e] = acc_b[e] = f2(0.0f);
                 for (int k = 0; k < kGroups; ++k) {
-                    acc_g[j] += s_col[(j * 2 + 0) * kCta + k * T + t];
-                    acc_b[j] += s_col[(j * 2 + 1) * kCta + k * T + t];
+                    const float *p = s_col + k * T + t;
+                    acc_g[e] = add2(acc_g[e], f2(p[(4 * e + 0) * kCta], p[(4 * e + 1) * kCta]));
+                    acc_b[e] = add2(acc_b[e], f2(p[(4 * e + 2) * kCta], p[(4 * e + 3) * kCta]));
                 }
             }
         }
     }
     if (g == 0) {
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            const int k = VEC ? col + j : col + j * T;
-            if (k < N) {
-                row[k] = acc_g[j];
-                row[N + k] = acc_b[j];
+        for (int e = 0; e < E; ++e)
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+                const int k = first(e >> 2) + (2 * (e & 3) + u) * kStep;
+                if (k < N) {
+                    row[k] = u ? hi(acc_g[e]) : lo(acc_g[e]);
+                    row[N + k] = u ? hi(acc_b[e]) : lo(acc_b[e]);
+                }
             }
-        }
     }
 }
 
-template <typename TX, typename TY, bool VEC, int T, int R, bool KEPT>
+template <typename TX, typename TY, bool VEC, int T, int C, int R, bool KEPT>
 cudaError_t launch_backward(const NormBackward &a, int n_sm, int *n_partials, cudaStream_t stream)
 {
     constexpr int kGroups = cta_threads(T) / T;
     const long long want = ((long long)a.M + kGroups * R - 1) / (kGroups * R);
-    long long most = (long long)n_sm * (cta_threads(T) > 256 ? 1 : 4);
+    long long most = (long long)n_sm * (512 / cta_threads(T));
     most = most < kNormMaxPartials ? most : kNormMaxPartials;
     const int grid = (int)(want < most ? want : most);
-    norm_backward_kernel<TX, TY, VEC, T, R, KEPT><<<grid, cta_threads(T), 0, stream>>>(a);
+    norm_backward_kernel<TX, TY, VEC, T, C, R, KEPT><<<grid, cta_threads(T), 0, stream>>>(a);
     *n_partials = grid;
     return cudaGetLastError();
 }
@@ -181,18 +239,18 @@ cudaError_t dispatch_width(const NormBackward &a, bool vec, int n_sm, int *n, cu
 {
     const int N = a.N;
     if (!vec) {
-        if (N <= 256) return launch_backward<TX, TY, false, 32, 2, KEPT>(a, n_sm, n, st);
-        if (N <= 1024) return launch_backward<TX, TY, false, 128, 2, KEPT>(a, n_sm, n, st);
-        return launch_backward<TX, TY, false, 1024, 1, KEPT>(a, n_sm, n, st);
+        if (N <= 256) return launch_backward<TX, TY, false, 32, 1, 2, KEPT>(a, n_sm, n, st);
+        if (N <= 1024) return launch_backward<TX, TY, false, 128, 1, 2, KEPT>(a, n_sm, n, st);
+        return launch_backward<TX, TY, false, 512, 2, 1, KEPT>(a, n_sm, n, st);
     }
-    if (N <= 64) return launch_backward<TX, TY, true, 8, 2, KEPT>(a, n_sm, n, st);
-    if (N <= 128) return launch_backward<TX, TY, true, 16, 2, KEPT>(a, n_sm, n, st);
-    if (N <= 256) return launch_backward<TX, TY, true, 32, 2, KEPT>(a, n_sm, n, st);
-    if (N <= 512) return launch_backward<TX, TY, true, 64, 2, KEPT>(a, n_sm, n, st);
-    if (N <= 1024) return launch_backward<TX, TY, true, 128, 2, KEPT>(a, n_sm, n, st);
-    if (N <= 2048) return launch_backward<TX, TY, true, 256, 2, KEPT>(a, n_sm, n, st);
-    if (N <= 4096) return launch_backward<TX, TY, true, 512, 2, KEPT>(a, n_sm, n, st);
-    return launch_backward<TX, TY, true, 1024, 1, KEPT>(a, n_sm, n, st);
+    if (N <= 64) return launch_backward<TX, TY, true, 8, 1, 2, KEPT>(a, n_sm, n, st);
+    if (N <= 128) return launch_backward<TX, TY, true, 16, 1, 2, KEPT>(a, n_sm, n, st);
+    if (N <= 256) return launch_backward<TX, TY, true, 32, 1, 2, KEPT>(a, n_sm, n, st);
+    if (N <= 512) return launch_backward<TX, TY, true, 64, 1, 2, KEPT>(a, n_sm, n, st);
+    if (N <= 1024) return launch_backward<TX, TY, true, 128, 1, 2, KEPT>(a, n_sm, n, st);
+    if (N <= 2048) return launch_backward<TX, TY, true, 256, 1, 2, KEPT>(a, n_sm, n, st);
+    if (N <= 4096) return launch_backward<TX, TY, true, 512, 1, 1, KEPT>(a, n_sm, n, st);
+    return launch_backward<TX, TY, true, 512, 2, 1, KEPT>(a, n_sm, n, st);
 }
 template <typename TX, typename TY>
 cudaError_t dispatch_source(const NormBackward &a, bool vec, int n_sm, int *n, cudaStream_t st)
