@@ -18,37 +18,39 @@ namespace {
 
 constexpr __host__ __device__ int cta_threads(int T) { return T > 256 ? T : 256; }
 
-// The sums of K values (a power of two, at most 4) over the T lanes of a row, or over a warp if T is more; in every lane.
+// The sums of K values (a power of two, at most 4) over the T lanes of a row (T < 32: in every lane), or over a warp: value
+// lane_value(lane) of them, in every lane.
 template <int T, int K>
-__device__ __forceinline__ void lane_sums(float (&s)[K])
+__device__ __forceinline__ float lane_sums(float (&s)[K])
 {
     constexpr unsigned kAll = 0xffffffffu;
-    if (T < 32 || K == 1) {
+    if (T < 32) {
 #pragma unroll
         for (int k = 0; k < K; ++k)
 #pragma unroll
-            for (int o = (T < 32 ? T : 32) / 2; o > 0; o >>= 1) s[k] += __shfl_xor_sync(kAll, s[k], o);
-        return;
+            for (int o = T / 2; o > 0; o >>= 1) s[k] += __shfl_xor_sync(kAll, s[k], o);
+        return 0.0f;
     }
-    // each half of the lanes goes on with one half of the values: K - 1 + (5 - log2 K) + K exchanges for K x 5
+    // each half of the lanes goes on with one half of the values: 6 exchanges for 4 values in place of 20
     const int lane = threadIdx.x & 31;
-    float a[2], one;
-    if (K == 4) {
-        const bool up = lane & 16;
 #pragma unroll
-        for (int k = 0; k < 2; ++k) {
-            const float keep = up ? s[2 + k] : s[k], send = up ? s[k] : s[2 + k];
-            a[k] = keep + __shfl_xor_sync(kAll, send, 16);
+    for (int n = K / 2, o = 16; n > 0; n /= 2, o /= 2) {
+        const bool up = lane & o;
+#pragma unroll
+        for (int k = 0; k < n; ++k) {
+            const float mine = up ? s[n + k] : s[k], other = up ? s[k] : s[n + k];
+            s[k] = mine + __shfl_xor_sync(kAll, other, o);
         }
-    } else { a[0] = s[0]; a[1] = s[K - 1]; }
-    constexpr int o2 = K == 4 ? 8 : 16;
-    const bool up = lane & o2;
-    one = (up ? a[1] : a[0]) + __shfl_xor_sync(kAll, up ? a[0] : a[1], o2);
+    }
+    float one = s[0];
 #pragma unroll
-    for (int o = o2 / 2; o > 0; o >>= 1) one += __shfl_xor_sync(kAll, one, o);
-#pragma unroll
-    for (int k = 0; k < K; ++k) s[k] = __shfl_sync(kAll, one, K == 4 ? (k >> 1) * 16 + (k & 1) * 8 : k * 16);
+    for (int o = 16 / K; o > 0; o >>= 1) one += __shfl_xor_sync(kAll, one, o);
+    return one;
 }
+template <int K>
+__device__ __forceinline__ int lane_value(int lane) { return lane / (32 / K); }
+template <int K>
+__device__ __forceinline__ bool lane_speaks(int lane) { return lane % (32 / K) == 0; }
 
 // T threads share a row; each owns C groups of eight columns: VEC neighbours, else every T-th.  A group of T threads takes R rows
 // at a time.
@@ -57,7 +59,7 @@ __global__ void __launch_bounds__(cta_threads(T), 512 / cta_threads(T)) norm_bac
 {
     constexpr int kCta = cta_threads(T), kGroups = kCta / T, E = 4 * C;
     constexpr int kWarps = T / 32;                                       // of a row (0: less than one)
-    __shared__ float s_red[2][kGroups][kWarps > 0 ? kWarps : 1][2 * R];
+    __shared__ __align__(16) float s_red[2][kGroups][kWarps > 0 ? kWarps : 1][2 * R];
     __shared__ float s_col[kGroups > 1 ? kCta * 16 : 1];
     const int t = threadIdx.x & (T - 1), g = threadIdx.x / T, N = P.N;
     const auto first = [&](int c) { return VEC ? (c * T + t) * 8 : c * 8 * T + t; };
@@ -81,24 +83,43 @@ __global__ void __launch_bounds__(cta_threads(T), 512 / cta_threads(T)) norm_bac
         Eight<TX> x[KEPT ? 1 : R][C];
         Eight<TY> y[R][C];
         uint2 code[KEPT ? R : 1][C];
-        uint32_t byte[KEPT && VEC ? R : 1][C];
+        uint32_t byte[KEPT ? R : 1][C];
         float mean[R], rstd[R];
     } raw;
+    // rows of a batch lie kGroups apart; most batches are whole and most rows end on a group of eight, and take the plain loads
+    const bool ragged = VEC ? (N & 7) != 0 : true;
     const auto load = [&](long long base) {
+        const bool whole = base + kGroups * R <= P.M && !ragged;
+        const long long r0 = base + g;
+        const TY *py = dy + r0 * P.ld_dy;
+        const TX *px = x + r0 * P.ldx;
+        const uint8_t *pc = P.kept.code + r0 * P.kept.ld_code, *ps = P.kept.scale + r0 * P.kept.ld_scale;
 #pragma unroll
         for (int i = 0; i < R; ++i) {
-            const long long r = base + (long long)i * kGroups + g;
-            const bool in = r < P.M;
+            const bool in = whole || r0 + (long long)i * kGroups < P.M;
 #pragma unroll
             for (int c = 0; c < C; ++c) {
-                raw.y[i][c] = in ? load8<VEC>(dy + r * P.ld_dy, first(c), T, N) : zero8(dy);
-                if (KEPT) {
-                    raw.code[i][c] = in ? load_codes8<VEC>(P.kept.code + r * P.kept.ld_code, first(c), T, N) : make_uint2(0u, 0u);
-                    if (VEC) raw.byte[i][c] = in && first(c) < N ? P.kept.scale[r * P.kept.ld_scale + (first(c) >> 5)] : 0u;
-                } else raw.x[i][c] = in ? load8<VEC>(x + r * P.ldx, first(c), T, N) : zero8(x);
+                if (whole) {
+                    const bool live = first(c) < N;
+                    raw.y[i][c] = live ? full8(py + first(c)) : zero8(dy);
+                    if (KEPT) {
+                        raw.code[i][c] = live ? __ldcs(reinterpret_cast<const uint2 *>(pc + first(c))) : make_uint2(0u, 0u);
+                        raw.byte[i][c] = live ? ps[first(c) >> 5] : 0u;
+                    } else raw.x[i][c] = live ? full8(px + first(c)) : zero8(x);
+                } else {
+                    raw.y[i][c] = in ? load8<VEC>(py, first(c), T, N) : zero8(dy);
+                    if (KEPT) {
+                        raw.code[i][c] = in ? load_codes8<VEC>(pc, first(c), T, N) : make_uint2(0u, 0u);
+                        if (VEC) raw.byte[i][c] = in && first(c) < N ? ps[first(c) >> 5] : 0u;
+                    } else raw.x[i][c] = in ? load8<VEC>(px, first(c), T, N) : zero8(x);
+                }
             }
-            raw.rstd[i] = in ? P.rstd[r] : 0.0f;
-            if (!KEPT) raw.mean[i] = in ? P.mean[r] : 0.0f;
+            raw.rstd[i] = in ? P.rstd[r0 + i * kGroups] : 0.0f;
+            if (!KEPT) raw.mean[i] = in ? P.mean[r0 + i * kGroups] : 0.0f;
+            py += kGroups * P.ld_dy;
+            px += kGroups * P.ldx;
+            pc += kGroups * P.kept.ld_code;
+            ps += kGroups * P.kept.ld_scale;
         }
     };
     const long long step = (long long)gridDim.x * kGroups * R;
@@ -150,26 +171,37 @@ __global__ void __launch_bounds__(cta_threads(T), 512 / cta_threads(T)) norm_bac
             s[2 * i] = lo(s1) + hi(s1);
             s[2 * i + 1] = lo(s2) + hi(s2);
         }
-        lane_sums<T>(s);
-        if (T > 32) {
-            if ((threadIdx.x & 31) == 0) {
+        const float one = lane_sums<T>(s);
+        if (T == 32) {
 #pragma unroll
-                for (int k = 0; k < 2 * R; ++k) s_red[buf][g][t >> 5][k] = s[k];
-            }
+            for (int k = 0; k < 2 * R; ++k) s[k] = __shfl_sync(0xffffffffu, one, k * (16 / R));
+        }
+        if (T > 32) {
+            const int lane = threadIdx.x & 31;
+            if (lane_speaks<2 * R>(lane)) s_red[buf][g][t >> 5][lane_value<2 * R>(lane)] = one;
             // the row group's own barrier (two buffers: nobody still reads the one that is written next)
             asm volatile("bar.sync %0, %1;" ::"r"(1 + g), "n"(T) : "memory");
 #pragma unroll
-            for (int k = 0; k < 2 * R; ++k) s[k] = 0.0f;
+            for (int w = 0; w < kWarps; ++w) {
+                float v[2 * R];
+                if (R == 2) {
+                    const float4 q = *reinterpret_cast<const float4 *>(s_red[buf][g][w]);
+                    v[0] = q.x; v[1] = q.y; v[2 * R - 2] = q.z; v[2 * R - 1] = q.w;
+                } else {
+                    const float2 q = *reinterpret_cast<const float2 *>(s_red[buf][g][w]);
+                    v[0] = q.x; v[1] = q.y;
+                }
 #pragma unroll
-            for (int w = 0; w < kWarps; ++w)
-#pragma unroll
-                for (int k = 0; k < 2 * R; ++k) s[k] += s_red[buf][g][w][k];
+                for (int k = 0; k < 2 * R; ++k) s[k] = w == 0 ? v[k] : s[k] + v[k];
+            }
             buf ^= 1;
         }
         if (dx) {
+            const long long r0 = base + g;
+            TX *pd = dx + r0 * P.ld_dx;
+            const bool whole = base + kGroups * R <= P.M && !ragged;
 #pragma unroll
             for (int i = 0; i < R; ++i) {
-                const long long r = base + (long long)i * kGroups + g;
                 const F2 minus_c1 = f2(-(s[2 * i] * inv_n)), minus_c2 = f2(-(s[2 * i + 1] * inv_n)), scale = f2(rstd[i]);
 #pragma unroll
                 for (int c = 0; c < C; ++c) {
@@ -179,8 +211,11 @@ __global__ void __launch_bounds__(cta_threads(T), 512 / cta_threads(T)) norm_bac
                         const int e = 4 * c + j;
                         out[j] = mul2(scale, fma2(xh[i][e], minus_c2, fma2(ga[e], h[i][e], minus_c1)));
                     }
-                    if (r < P.M) store8<VEC, false>(dx + r * P.ld_dx, first(c), T, N, out);
+                    if (whole) {
+                        if (first(c) < N) full_store8<false>(pd + first(c), out);
+                    } else if (r0 + (long long)i * kGroups < P.M) store8<VEC, false>(pd, first(c), T, N, out);
                 }
+                pd += kGroups * P.ld_dx;
             }
         }
     }
