@@ -54,7 +54,7 @@ __device__ __forceinline__ bool lane_speaks(int lane) { return lane % (32 / K) =
 
 // T threads share a row; each owns C groups of eight columns: VEC neighbours, else every T-th.  A group of T threads takes R rows
 // at a time.
-template <typename TX, typename TY, bool VEC, int T, int C, int R, bool KEPT>
+template <typename TX, typename TY, bool VEC, int T, int C, int R, bool KEPT, bool RELU>
 __global__ void __launch_bounds__(cta_threads(T), 512 / cta_threads(T)) norm_backward_kernel(const NormBackward P)
 {
     constexpr int kCta = cta_threads(T), kGroups = kCta / T, E = 4 * C;
@@ -67,13 +67,13 @@ __global__ void __launch_bounds__(cta_threads(T), 512 / cta_threads(T)) norm_bac
     const TX *x = static_cast<const TX *>(P.x);
     TX *dx = static_cast<TX *>(P.dx);
     const TY *dy = static_cast<const TY *>(P.dy);
-    F2 ga[E], be[E], acc_g[E], acc_b[E];
+    F2 ga[E], be[RELU ? E : 1], acc_g[E], acc_b[E];
 #pragma unroll
     for (int i = 0; i < E; ++i) {
         const int k = first(i >> 2) + 2 * (i & 3) * kStep;
         const auto at = [&](const float *p, int c, float other) { return c >= N ? 0.0f : p ? __ldg(p + c) : other; };
         ga[i] = f2(at(P.gamma, k, 1.0f), at(P.gamma, k + kStep, 1.0f));
-        be[i] = f2(at(P.beta, k, 0.0f), at(P.beta, k + kStep, 0.0f));
+        if (RELU) be[i] = f2(at(P.beta, k, 0.0f), at(P.beta, k + kStep, 0.0f));
         acc_g[i] = acc_b[i] = f2(0.0f);
     }
     const float inv_n = 1.0f / (float)N;
@@ -86,40 +86,32 @@ __global__ void __launch_bounds__(cta_threads(T), 512 / cta_threads(T)) norm_bac
         uint32_t byte[KEPT ? R : 1][C];
         float mean[R], rstd[R];
     } raw;
-    // rows of a batch lie kGroups apart; most batches are whole and most rows end on a group of eight, and take the plain loads
-    const bool ragged = VEC ? (N & 7) != 0 : true;
+    // Nothing is asked for under a condition (a load under one would be waited for where the branches meet): rows behind the last are
+    // the last one again, columns behind the last (VEC: whole groups of them) the first, and neither enters a sum or an output.
     const auto load = [&](long long base) {
-        const bool whole = base + kGroups * R <= P.M && !ragged;
-        const long long r0 = base + g;
-        const TY *py = dy + r0 * P.ld_dy;
-        const TX *px = x + r0 * P.ldx;
-        const uint8_t *pc = P.kept.code + r0 * P.kept.ld_code, *ps = P.kept.scale + r0 * P.kept.ld_scale;
 #pragma unroll
         for (int i = 0; i < R; ++i) {
-            const bool in = whole || r0 + (long long)i * kGroups < P.M;
+            const long long r = min(base + (long long)i * kGroups + g, (long long)P.M - 1);
+            const TY *py = dy + r * P.ld_dy;
+            const TX *px = x + r * P.ldx;
+            const uint8_t *pc = P.kept.code + r * P.kept.ld_code, *ps = P.kept.scale + r * P.kept.ld_scale;
 #pragma unroll
             for (int c = 0; c < C; ++c) {
-                if (whole) {
-                    const bool live = first(c) < N;
-                    raw.y[i][c] = live ? full8(py + first(c)) : zero8(dy);
+                if (VEC) {
+                    const int col = first(c) < N ? first(c) : 0;
+                    raw.y[i][c] = full8(py + col);
                     if (KEPT) {
-                        raw.code[i][c] = live ? __ldcs(reinterpret_cast<const uint2 *>(pc + first(c))) : make_uint2(0u, 0u);
-                        raw.byte[i][c] = live ? ps[first(c) >> 5] : 0u;
-                    } else raw.x[i][c] = live ? full8(px + first(c)) : zero8(x);
+                        raw.code[i][c] = __ldcs(reinterpret_cast<const uint2 *>(pc + col));
+                        raw.byte[i][c] = ps[col >> 5];
+                    } else raw.x[i][c] = full8(px + col);
                 } else {
-                    raw.y[i][c] = in ? load8<VEC>(py, first(c), T, N) : zero8(dy);
-                    if (KEPT) {
-                        raw.code[i][c] = in ? load_codes8<VEC>(pc, first(c), T, N) : make_uint2(0u, 0u);
-                        if (VEC) raw.byte[i][c] = in && first(c) < N ? ps[first(c) >> 5] : 0u;
-                    } else raw.x[i][c] = in ? load8<VEC>(px, first(c), T, N) : zero8(x);
+                    raw.y[i][c] = load8<false>(py, first(c), T, N);
+                    if (KEPT) raw.code[i][c] = load_codes8<false>(pc, first(c), T, N);
+                    else raw.x[i][c] = load8<false>(px, first(c), T, N);
                 }
             }
-            raw.rstd[i] = in ? P.rstd[r0 + i * kGroups] : 0.0f;
-            if (!KEPT) raw.mean[i] = in ? P.mean[r0 + i * kGroups] : 0.0f;
-            py += kGroups * P.ld_dy;
-            px += kGroups * P.ldx;
-            pc += kGroups * P.kept.ld_code;
-            ps += kGroups * P.kept.ld_scale;
+            raw.rstd[i] = P.rstd[r];
+            if (!KEPT) raw.mean[i] = P.mean[r];
         }
     };
     const long long step = (long long)gridDim.x * kGroups * R;
@@ -152,13 +144,21 @@ __global__ void __launch_bounds__(cta_threads(T), 512 / cta_threads(T)) norm_bac
                 }
             }
         }
-        if (base + step < P.M) load(base + step);
+        load(base + step);
+        if (base + kGroups * R > P.M) {                                   // the last batch: rows that are none
+#pragma unroll
+            for (int i = 0; i < R; ++i)
+                if (base + (long long)i * kGroups + g >= P.M) {
+#pragma unroll
+                    for (int e = 0; e < E; ++e) h[i][e] = f2(0.0f);
+                }
+        }
 #pragma unroll
         for (int i = 0; i < R; ++i) {
             F2 s1 = f2(0.0f), s2 = f2(0.0f);
 #pragma unroll
             for (int e = 0; e < E; ++e) {
-                if (P.relu) {
+                if (RELU) {
                     const F2 y = fma2(ga[e], xh[i][e], be[e]);
                     h[i][e] = f2(lo(y) > 0.0f ? lo(h[i][e]) : 0.0f, hi(y) > 0.0f ? hi(h[i][e]) : 0.0f);
                 }
@@ -199,7 +199,6 @@ __global__ void __launch_bounds__(cta_threads(T), 512 / cta_threads(T)) norm_bac
         if (dx) {
             const long long r0 = base + g;
             TX *pd = dx + r0 * P.ld_dx;
-            const bool whole = base + kGroups * R <= P.M && !ragged;
 #pragma unroll
             for (int i = 0; i < R; ++i) {
                 const F2 minus_c1 = f2(-(s[2 * i] * inv_n)), minus_c2 = f2(-(s[2 * i + 1] * inv_n)), scale = f2(rstd[i]);
@@ -211,9 +210,10 @@ __global__ void __launch_bounds__(cta_threads(T), 512 / cta_threads(T)) norm_bac
                         const int e = 4 * c + j;
                         out[j] = mul2(scale, fma2(xh[i][e], minus_c2, fma2(ga[e], h[i][e], minus_c1)));
                     }
-                    if (whole) {
-                        if (first(c) < N) full_store8<false>(pd + first(c), out);
-                    } else if (r0 + (long long)i * kGroups < P.M) store8<VEC, false>(pd, first(c), T, N, out);
+                    if (r0 + (long long)i * kGroups < P.M && first(c) < N) {
+                        if (VEC) full_store8<false>(pd + first(c), out);
+                        else store8<false, false>(pd, first(c), T, N, out);
+                    }
                 }
                 pd += kGroups * P.ld_dx;
             }
@@ -257,7 +257,7 @@ __global__ void __launch_bounds__(cta_threads(T), 512 / cta_threads(T)) norm_bac
     }
 }
 
-template <typename TX, typename TY, bool VEC, int T, int C, int R, bool KEPT>
+template <typename TX, typename TY, bool VEC, int T, int C, int R, bool KEPT, bool RELU>
 cudaError_t launch_backward(const NormBackward &a, int n_sm, int *n_partials, cudaStream_t stream)
 {
     constexpr int kGroups = cta_threads(T) / T;
@@ -265,39 +265,39 @@ cudaError_t launch_backward(const NormBackward &a, int n_sm, int *n_partials, cu
     long long most = (long long)n_sm * (512 / cta_threads(T));
     most = most < kNormMaxPartials ? most : kNormMaxPartials;
     const int grid = (int)(want < most ? want : most);
-    norm_backward_kernel<TX, TY, VEC, T, C, R, KEPT><<<grid, cta_threads(T), 0, stream>>>(a);
+    norm_backward_kernel<TX, TY, VEC, T, C, R, KEPT, RELU><<<grid, cta_threads(T), 0, stream>>>(a);
     *n_partials = grid;
     return cudaGetLastError();
 }
-template <typename TX, typename TY, bool KEPT>
+template <typename TX, typename TY, bool KEPT, bool RELU>
 cudaError_t dispatch_width(const NormBackward &a, bool vec, int n_sm, int *n, cudaStream_t st)
 {
     const int N = a.N;
     if (!vec) {
-        if (N <= 256) return launch_backward<TX, TY, false, 32, 1, 2, KEPT>(a, n_sm, n, st);
-        if (N <= 1024) return launch_backward<TX, TY, false, 128, 1, 2, KEPT>(a, n_sm, n, st);
-        return launch_backward<TX, TY, false, 512, 2, 1, KEPT>(a, n_sm, n, st);
+        if (N <= 256) return launch_backward<TX, TY, false, 32, 1, 2, KEPT, RELU>(a, n_sm, n, st);
+        if (N <= 1024) return launch_backward<TX, TY, false, 128, 1, 2, KEPT, RELU>(a, n_sm, n, st);
+        return launch_backward<TX, TY, false, 512, 2, 1, KEPT, RELU>(a, n_sm, n, st);
     }
-    if (N <= 64) return launch_backward<TX, TY, true, 8, 1, 2, KEPT>(a, n_sm, n, st);
-    if (N <= 128) return launch_backward<TX, TY, true, 16, 1, 2, KEPT>(a, n_sm, n, st);
-    if (N <= 256) return launch_backward<TX, TY, true, 32, 1, 2, KEPT>(a, n_sm, n, st);
-    if (N <= 512) return launch_backward<TX, TY, true, 64, 1, 2, KEPT>(a, n_sm, n, st);
-    if (N <= 1024) return launch_backward<TX, TY, true, 128, 1, 2, KEPT>(a, n_sm, n, st);
-    if (N <= 2048) return launch_backward<TX, TY, true, 256, 1, 2, KEPT>(a, n_sm, n, st);
-    if (N <= 4096) return launch_backward<TX, TY, true, 512, 1, 1, KEPT>(a, n_sm, n, st);
-    return launch_backward<TX, TY, true, 512, 2, 1, KEPT>(a, n_sm, n, st);
+    if (N <= 64) return launch_backward<TX, TY, true, 8, 1, 2, KEPT, RELU>(a, n_sm, n, st);
+    if (N <= 256) return launch_backward<TX, TY, true, 32, 1, 2, KEPT, RELU>(a, n_sm, n, st);
+    if (N <= 512) return launch_backward<TX, TY, true, 64, 1, 2, KEPT, RELU>(a, n_sm, n, st);
+    if (N <= 1024) return launch_backward<TX, TY, true, 128, 1, 2, KEPT, RELU>(a, n_sm, n, st);
+    if (N <= 2048) return launch_backward<TX, TY, true, 256, 1, 2, KEPT, RELU>(a, n_sm, n, st);
+    if (N <= 4096) return launch_backward<TX, TY, true, 512, 1, 1, KEPT, RELU>(a, n_sm, n, st);
+    return launch_backward<TX, TY, true, 512, 2, 1, KEPT, RELU>(a, n_sm, n, st);
 }
 template <typename TX, typename TY>
 cudaError_t dispatch_source(const NormBackward &a, bool vec, int n_sm, int *n, cudaStream_t st)
 {
-    return a.x ? dispatch_width<TX, TY, false>(a, vec, n_sm, n, st) : dispatch_width<TX, TY, true>(a, vec, n_sm, n, st);
+    if (a.relu) return a.x ? dispatch_width<TX, TY, false, true>(a, vec, n_sm, n, st) : dispatch_width<TX, TY, true, true>(a, vec, n_sm, n, st);
+    return a.x ? dispatch_width<TX, TY, false, false>(a, vec, n_sm, n, st) : dispatch_width<TX, TY, true, false>(a, vec, n_sm, n, st);
 }
 
 }  // namespace
 
 cudaError_t launch_norm_backward(const NormBackward &a, int x_dtype, int dy_dtype, int n_sm, int *n_partials, cudaStream_t stream)
 {
-    const bool vec = rows_aligned16(a.dy, a.ld_dy, dy_dtype) && (!a.dx || rows_aligned16(a.dx, a.ld_dx, x_dtype)) &&
+    const bool vec = a.N % 8 == 0 && rows_aligned16(a.dy, a.ld_dy, dy_dtype) && (!a.dx || rows_aligned16(a.dx, a.ld_dx, x_dtype)) &&
                      (a.x ? rows_aligned16(a.x, a.ldx, x_dtype) : codes_aligned8(a.kept));
     if (x_dtype == IM_DTYPE_F32)
         return dy_dtype == IM_DTYPE_F32 ? dispatch_source<float, float>(a, vec, n_sm, n_partials, stream)
