@@ -87,20 +87,38 @@ __device__ __forceinline__ float act8_scale(uint32_t byte) { return __uint_as_fl
 __device__ __forceinline__ float act8_inverse(uint32_t byte) { return __uint_as_float((254u - byte) << 23); }
 
 __device__ __forceinline__ uint32_t abs_bits(float x) { return __float_as_uint(x) & 0x7fffffffu; }
-
-// Codes of four values already divided by 2^e (zeros for a block marked 255), lowest byte first.
-__device__ __forceinline__ uint32_t act8_encode4(float a, float b, float c, float d, int form)
+__device__ __forceinline__ uint32_t abs_bits_max8(const F2 *v)
 {
+    uint32_t m = __vimax3_u32(abs_bits(lo(v[0])), abs_bits(hi(v[0])), abs_bits(lo(v[1])));
+    m = __vimax3_u32(m, abs_bits(hi(v[1])), abs_bits(lo(v[2])));
+    m = __vimax3_u32(m, abs_bits(hi(v[2])), abs_bits(lo(v[3])));
+    return max(m, abs_bits(hi(v[3])));
+}
+
+// Codes of eight values, lowest byte first, under the scale byte that is theirs.
+__device__ __forceinline__ uint2 act8_encode8(const F2 *v, uint32_t byte, int form)
+{
+    const F2 inv = f2(act8_inverse(byte));
+    uint2 w;
     if (form == IM_ACT8_INT8) {
-        // 1.5 x 2^23 + v: the sum's low byte is the integer nearest to v, in two's complement
-        const uint32_t p = __float_as_uint(a + 12582912.0f), q = __float_as_uint(b + 12582912.0f);
-        const uint32_t r = __float_as_uint(c + 12582912.0f), s = __float_as_uint(d + 12582912.0f);
-        return __byte_perm(__byte_perm(p, q, 0x0040), __byte_perm(r, s, 0x0040), 0x5410);
+        // 1.5 x 2^23 + value / 2^e (one rounding, the division is exact): the sum's low byte is the nearest integer, in two's complement
+        F2 q[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) q[i] = fma2(v[i], inv, f2(12582912.0f));
+        const auto pack = [](F2 a, F2 b) {
+            return __byte_perm(__byte_perm(__float_as_uint(lo(a)), __float_as_uint(hi(a)), 0x0040), __byte_perm(__float_as_uint(lo(b)), __float_as_uint(hi(b)), 0x0040), 0x5410);
+        };
+        w = make_uint2(pack(q[0], q[1]), pack(q[2], q[3]));
+    } else {
+        uint16_t h[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const F2 q = mul2(v[i], inv);
+            asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(h[i]) : "f"(hi(q)), "f"(lo(q)));
+        }
+        w = make_uint2((uint32_t)h[0] | ((uint32_t)h[1] << 16), (uint32_t)h[2] | ((uint32_t)h[3] << 16));
     }
-    uint16_t lo, hi;
-    asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(lo) : "f"(b), "f"(a));
-    asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(hi) : "f"(d), "f"(c));
-    return (uint32_t)lo | ((uint32_t)hi << 16);
+    return byte == 255u ? make_uint2(0u, 0u) : w;
 }
 // The numbers that four codes stand for, without their scale.
 template <int FORM>
@@ -247,36 +265,29 @@ __device__ __forceinline__ void store_codes8(uint8_t *row, int col, int step, in
 template <bool SIDE, bool ALIGNED, int T>
 __device__ __forceinline__ void keep8(const Act8View &k, bool in, long long row, int col, int cols, const F2 *v)
 {
-    const auto at = [&](int j) { return j & 1 ? hi(v[j >> 1]) : lo(v[j >> 1]); };
-    float q[8];
     if (SIDE) {
-        uint32_t amax = 0u;
-#pragma unroll
-        for (int j = 0; j < 8; ++j) amax = max(amax, col + j < cols ? abs_bits(at(j)) : 0u);
+        // (values behind the last column are zeros)
+        uint32_t amax = abs_bits_max8(v);
         amax = max(amax, __shfl_xor_sync(0xffffffffu, amax, 1));
         amax = max(amax, __shfl_xor_sync(0xffffffffu, amax, 2));
         const uint32_t byte = act8_scale_byte(amax, k.form);
-        const F2 inv = f2(byte == 255u ? 0.0f : act8_inverse(byte));
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const F2 x = mul2(v[i], inv);
-            q[2 * i] = byte == 255u ? 0.0f : lo(x);
-            q[2 * i + 1] = byte == 255u ? 0.0f : hi(x);
-        }
+        const uint2 w = act8_encode8(v, byte, k.form);
         if (!in || col >= cols) return;
         if ((col & 31) == 0) k.scale[row * k.ld_scale + (col >> 5)] = (uint8_t)byte;
+        store_codes8<ALIGNED>(k.code + row * k.ld_code, col, 1, cols, w);
     } else {
+        uint32_t w[2] = {0u, 0u};
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
             const int c = col + j * T;
-            const uint32_t byte = act8_scale_byte(__reduce_max_sync(0xffffffffu, c < cols ? abs_bits(at(j)) : 0u), k.form);
-            q[j] = byte == 255u ? 0.0f : at(j) * act8_inverse(byte);
+            const float x = j & 1 ? hi(v[j >> 1]) : lo(v[j >> 1]);
+            const uint32_t byte = act8_scale_byte(__reduce_max_sync(0xffffffffu, abs_bits(x)), k.form);
             if (in && (c & 31) == 0 && c < cols) k.scale[row * k.ld_scale + (c >> 5)] = (uint8_t)byte;
+            const F2 one[4] = {f2(x, 0.0f), f2(0.0f), f2(0.0f), f2(0.0f)};
+            w[j >> 2] |= (act8_encode8(one, byte, k.form).x & 255u) << (8 * (j & 3));
         }
-        if (!in) return;
+        if (in) store_codes8<false>(k.code + row * k.ld_code, col, T, cols, make_uint2(w[0], w[1]));
     }
-    store_codes8<SIDE && ALIGNED>(k.code + row * k.ld_code, col, SIDE ? 1 : T, cols,
-                                  make_uint2(act8_encode4(q[0], q[1], q[2], q[3], k.form), act8_encode4(q[4], q[5], q[6], q[7], k.form)));
 }
 
 inline bool aligned_to(const void *p, uintptr_t bytes) { return (reinterpret_cast<uintptr_t>(p) & (bytes - 1)) == 0; }

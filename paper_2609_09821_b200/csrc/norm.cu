@@ -161,6 +161,8 @@ cudaError_t dispatch_forward(const NormForward &a, bool vec, int n_sm, cudaStrea
     const int N = a.N;
     if (!vec) {
         if (N <= 256) return launch_forward<TX, TY, false, 32, 1>(a, n_sm, st);
+        if (N <= 512) return launch_forward<TX, TY, false, 32, 2>(a, n_sm, st);
+        if (N <= 768) return launch_forward<TX, TY, false, 32, 3>(a, n_sm, st);
         if (N <= 1024) return launch_forward<TX, TY, false, 32, 4>(a, n_sm, st);
         return launch_forward<TX, TY, false, 256, 4>(a, n_sm, st);
     }
@@ -168,6 +170,7 @@ cudaError_t dispatch_forward(const NormForward &a, bool vec, int n_sm, cudaStrea
     if (N <= 128) return launch_forward<TX, TY, true, 16, 1>(a, n_sm, st);
     if (N <= 256) return launch_forward<TX, TY, true, 32, 1>(a, n_sm, st);
     if (N <= 512) return launch_forward<TX, TY, true, 32, 2>(a, n_sm, st);
+    if (N <= 768) return launch_forward<TX, TY, true, 32, 3>(a, n_sm, st);
     if (N <= 1024) return launch_forward<TX, TY, true, 32, 4>(a, n_sm, st);
     if (N <= 2048) return launch_forward<TX, TY, true, 256, 1>(a, n_sm, st);
     if (N <= 4096) return launch_forward<TX, TY, true, 256, 2>(a, n_sm, st);
