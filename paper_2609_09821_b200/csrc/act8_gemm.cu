@@ -441,6 +441,7 @@ __device__ __forceinline__ void act8_tn_body(const CUtensorMap &map_a, const CUt
             }
         }
     }
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");      // (the kernel that adds partial tiles waits for this one's end)
     // everyone meets (in a pair, so that shared memory and barriers outlive the peer's use of them); the allocating warp frees tensor memory
     if (*abort_flag && lane == 0) {
         // a wait ran out: copies and MMAs in flight get time to land (bounded)
@@ -470,20 +471,34 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) act8_tn
     act8_tn_body<256, true, FORM, MODE>(map_a, map_h, P);
 }
 
-// C = the partial tiles, added in a fixed order (slices, then helpers): a warp per 128 columns of one row.
-template <int BLOCK_N, bool PAIR>
+// C = the partial tiles, added in a fixed order (slices, then helpers).  A warp has 128 columns of a row; with SPLIT the eight warps of a
+// CTA share one row's parts, every eighth each, and their sums are added in order: few tiles have many parts.
+// Launched early (programmatically): it waits for the products, and reads what they wrote by plain loads.
+constexpr int kSplitFrom = 12;             // slices
+template <int BLOCK_N, bool PAIR, bool SPLIT>
 __global__ void __launch_bounds__(256) act8_tn_finish_kernel(const Act8GemmParams P)
 {
+    asm volatile("griddepcontrol.wait;" ::: "memory");
     using PL = Plan<BLOCK_N, PAIR>;
     constexpr long long kSlot = (long long)BLOCK_N * PL::kCols;
-    const int n = (int)blockIdx.y * 8 + (threadIdx.x >> 5), k = (int)blockIdx.x * 128 + (threadIdx.x & 31) * 4;
+    __shared__ float4 s_part[SPLIT ? 8 : 1][32];
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int n = SPLIT ? (int)blockIdx.y : (int)blockIdx.y * 8 + warp, k = (int)blockIdx.x * 128 + lane * 4;
     if (n >= P.Mo) return;
     const int tile = n / BLOCK_N * P.tiles_k + k / PL::kCols;
     const float *src = P.partial + (long long)(n % BLOCK_N) * PL::kCols + k % PL::kCols;
-    const auto at = [&](long long slot) { return __ldg(reinterpret_cast<const float4 *>(src + slot * kSlot)); };
-    float4 sum = at((long long)tile * P.slices);
+    const auto at = [&](long long slot) { return __ldcg(reinterpret_cast<const float4 *>(src + slot * kSlot)); };
+    float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
     const auto add = [&](const float4 &v) { sum.x += v.x; sum.y += v.y; sum.z += v.z; sum.w += v.w; };
-    for (int s = 1; s < P.slices; ++s) add(at((long long)tile * P.slices + s));
+#pragma unroll 4
+    for (int s = SPLIT ? warp : 0; s < P.slices; s += SPLIT ? 8 : 1) add(at((long long)tile * P.slices + s));
+    if (SPLIT) {
+        s_part[warp][lane] = sum;
+        __syncthreads();
+        if (warp) return;
+#pragma unroll
+        for (int w = 1; w < 8; ++w) add(s_part[w][lane]);
+    }
     if (P.helpers) {
         const int rest = P.kb - P.slices * P.slice_kb;
         const long long units = (long long)P.tiles * rest, u0 = (long long)tile * rest, u1 = u0 + rest;
@@ -498,6 +513,13 @@ __global__ void __launch_bounds__(256) act8_tn_finish_kernel(const Act8GemmParam
     if (k + 1 < P.No) dst[1] = sum.y;
     if (k + 2 < P.No) dst[2] = sum.z;
     if (k + 3 < P.No) dst[3] = sum.w;
+}
+template <int BLOCK_N, bool PAIR>
+cudaError_t launch_finish(const Act8GemmParams &p, cudaStream_t st)
+{
+    const unsigned gx = (unsigned)((p.No + 127) / 128);
+    if (p.slices >= kSplitFrom) return launch_pdl(act8_tn_finish_kernel<BLOCK_N, PAIR, true>, dim3(gx, (unsigned)p.Mo), dim3(256), 0, st, 0, p);
+    return launch_pdl(act8_tn_finish_kernel<BLOCK_N, PAIR, false>, dim3(gx, (unsigned)((p.Mo + 7) / 8)), dim3(256), 0, st, 0, p);
 }
 
 // Tile shape and split.  Narrow A: one CTA per tile, 64 or 128 columns; else pairs with 256, unless H is too narrow for both CTAs.
@@ -612,12 +634,8 @@ im_status im_gemm_act8_tn(const uint16_t *A, int64_t lda, const im_act8 *H, floa
     cudaError_t e = H->form == IM_ACT8_INT8 ? launch_product<IM_ACT8_INT8>(s, map, map_h, p, mode, grid, st) : launch_product<IM_ACT8_E4M3>(s, map, map_h, p, mode, grid, st);
     g_launches.fetch_add(1, std::memory_order_relaxed);
     if (e == cudaSuccess && p.partial) {
-        const dim3 fin((unsigned)((No + 127) / 128), (unsigned)((Mo + 7) / 8));
-        if (s.pair) act8_tn_finish_kernel<256, true><<<fin, 256, 0, st>>>(p);
-        else if (s.block_n == 64) act8_tn_finish_kernel<64, false><<<fin, 256, 0, st>>>(p);
-        else act8_tn_finish_kernel<128, false><<<fin, 256, 0, st>>>(p);
+        e = s.pair ? launch_finish<256, true>(p, st) : s.block_n == 64 ? launch_finish<64, false>(p, st) : launch_finish<128, false>(p, st);
         g_launches.fetch_add(1, std::memory_order_relaxed);
-        e = cudaGetLastError();
     }
     return e == cudaSuccess ? IM_OK : IM_ERR_CUDA;
 }

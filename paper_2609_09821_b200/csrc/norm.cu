@@ -113,15 +113,18 @@ __global__ void __launch_bounds__(kThreads) norm_forward_kernel(const NormForwar
     }
 }
 
-// Column sums of the backward pass: the partial rows in fp64, sixteen threads a column, added in a fixed order.
-constexpr int kFinishParts = 16;
+// Column sums of the backward pass: the partial rows in fp64, 32 threads a column with their loads in flight together, added in a
+// fixed order.  Launched early (programmatically): it waits for the backward kernel, and reads what that wrote by plain loads.
+constexpr int kFinishParts = 32;
 __global__ void __launch_bounds__(32 * kFinishParts) norm_finish_kernel(const float *partial, int n_partials, int N, float *dgamma, float *dbeta)
 {
+    asm volatile("griddepcontrol.wait;" ::: "memory");
     __shared__ double part[kFinishParts][33];
     const int c = blockIdx.x * 32 + threadIdx.x;                          // of [dgamma | dbeta]
     double s = 0.0;
     if (c < 2 * N)
-        for (int i = threadIdx.y; i < n_partials; i += kFinishParts) s += (double)partial[(long long)i * 2 * N + c];
+#pragma unroll 4
+        for (int i = threadIdx.y; i < n_partials; i += kFinishParts) s += (double)__ldcg(partial + (long long)i * 2 * N + c);
     part[threadIdx.y][threadIdx.x] = s;
     __syncthreads();
     if (threadIdx.y == 0 && c < 2 * N) {
@@ -239,9 +242,8 @@ im_status im_layer_norm_backward(int32_t M, int32_t N, const void *dy, int64_t l
     cudaError_t e = launch_norm_backward(a, x_dtype, dy_dtype, n_sm, &n_partials, st);
     g_launches.fetch_add(1, std::memory_order_relaxed);
     if (e == cudaSuccess && sums) {
-        norm_finish_kernel<<<(2 * N + 31) / 32, dim3(32, kFinishParts), 0, st>>>(a.partial, n_partials, N, dgamma, dbeta);
+        e = launch_pdl(norm_finish_kernel, dim3((unsigned)((2 * N + 31) / 32)), dim3(32, kFinishParts), 0, st, 0, (const float *)a.partial, n_partials, N, dgamma, dbeta);
         g_launches.fetch_add(1, std::memory_order_relaxed);
-        e = cudaGetLastError();
     }
     return e == cudaSuccess ? IM_OK : IM_ERR_CUDA;
 }

@@ -219,6 +219,7 @@ __global__ void __launch_bounds__(cta_threads(T), 512 / cta_threads(T)) norm_bac
             }
         }
     }
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");      // (the kernel that adds the partial sums waits for this one's end)
     if (!P.partial) return;
     float *row = P.partial + (long long)blockIdx.x * 2 * N;
     if (kGroups > 1) {
