@@ -20,6 +20,7 @@ __global__ void __launch_bounds__(kThreads, 4) pack_kernel(const T *x, long long
     const int tx = threadIdx.x & ((1 << tx_bits) - 1), ty = threadIdx.x >> tx_bits, rows_per_cta = kThreads >> tx_bits;
     const int col = VEC ? (((int)blockIdx.x << tx_bits) + tx) * 8 : (int)blockIdx.x * 8 * kStride + tx;
     const long long row_step = (long long)gridDim.y * rows_per_cta;
+    after_previous_kernel();
     // (whole warps run together: the maximum is taken across the lanes of a row)
     for (long long r0 = (long long)blockIdx.y * rows_per_cta; r0 < M; r0 += row_step * kRows) {
         Eight<T> raw[kRows];
@@ -46,9 +47,10 @@ __global__ void __launch_bounds__(kThreads, 4) unpack_kernel(const Act8View in, 
     const int tx = threadIdx.x & ((1 << tx_bits) - 1), ty = threadIdx.x >> tx_bits, rows_per_cta = kThreads >> tx_bits;
     const int col = VEC ? (((int)blockIdx.x << tx_bits) + tx) * 8 : (int)blockIdx.x * 8 * kStride + tx;
     const long long row_step = (long long)gridDim.y * rows_per_cta;
+    after_previous_kernel();
     F2 g[4], b[4];
     if (AFFINE) {
-        const auto at = [&](const float *p, int k, float other) { return p && k < N ? __ldg(p + k) : other; };
+        const auto at = [&](const float *p, int k, float other) { return p && k < N ? p[k] : other; };
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
             const int k = col + 2 * j * kStep;
@@ -128,17 +130,18 @@ im_status im_act8_pack(int32_t M, int32_t N, const void *x, int64_t ldx, int32_t
     const int bits = row_threads_bits(N, vec);
     const dim3 grid = grid_for(M, N, bits, x_dtype == IM_DTYPE_F32 ? 2 : 4, n_sm);
     cudaStream_t st = (cudaStream_t)cuda_stream;
+    cudaError_t e;
     const float *xf = static_cast<const float *>(x);
     const __nv_bfloat16 *xb = static_cast<const __nv_bfloat16 *>(x);
     if (x_dtype == IM_DTYPE_F32) {
-        if (vec) pack_kernel<float, true><<<grid, kThreads, 0, st>>>(xf, ldx, M, N, v, bits);
-        else pack_kernel<float, false><<<grid, kThreads, 0, st>>>(xf, ldx, M, N, v, bits);
+        if (vec) e = launch_pdl(pack_kernel<float, true>, grid, dim3(kThreads), 0, st, 0, xf, (long long)ldx, M, N, v, bits);
+        else e = launch_pdl(pack_kernel<float, false>, grid, dim3(kThreads), 0, st, 0, xf, (long long)ldx, M, N, v, bits);
     } else {
-        if (vec) pack_kernel<__nv_bfloat16, true><<<grid, kThreads, 0, st>>>(xb, ldx, M, N, v, bits);
-        else pack_kernel<__nv_bfloat16, false><<<grid, kThreads, 0, st>>>(xb, ldx, M, N, v, bits);
+        if (vec) e = launch_pdl(pack_kernel<__nv_bfloat16, true>, grid, dim3(kThreads), 0, st, 0, xb, (long long)ldx, M, N, v, bits);
+        else e = launch_pdl(pack_kernel<__nv_bfloat16, false>, grid, dim3(kThreads), 0, st, 0, xb, (long long)ldx, M, N, v, bits);
     }
     g_launches.fetch_add(1, std::memory_order_relaxed);
-    return cudaGetLastError() == cudaSuccess ? IM_OK : IM_ERR_CUDA;
+    return e == cudaSuccess ? IM_OK : IM_ERR_CUDA;
 }
 
 im_status im_act8_unpack(int32_t M, int32_t N, const im_act8 *in, const float *gamma, const float *beta, int32_t relu, void *out, int64_t ld_out,
@@ -153,10 +156,11 @@ im_status im_act8_unpack(int32_t M, int32_t N, const im_act8 *in, const float *g
     const int bits = row_threads_bits(N, vec);
     const dim3 grid = grid_for(M, N, bits, 4, n_sm);
     cudaStream_t st = (cudaStream_t)cuda_stream;
+    cudaError_t e;
 #define IM_UNPACK(T, VEC)                                                                                                                     \
     do {                                                                                                                                      \
-        if (affine) unpack_kernel<T, VEC, true><<<grid, kThreads, 0, st>>>(v, M, N, gamma, beta, relu, static_cast<T *>(out), ld_out, bits);   \
-        else unpack_kernel<T, VEC, false><<<grid, kThreads, 0, st>>>(v, M, N, nullptr, nullptr, 0, static_cast<T *>(out), ld_out, bits);       \
+        if (affine) e = launch_pdl(unpack_kernel<T, VEC, true>, grid, dim3(kThreads), 0, st, 0, v, M, N, gamma, beta, relu, static_cast<T *>(out), (long long)ld_out, bits); \
+        else e = launch_pdl(unpack_kernel<T, VEC, false>, grid, dim3(kThreads), 0, st, 0, v, M, N, (const float *)nullptr, (const float *)nullptr, 0, static_cast<T *>(out), (long long)ld_out, bits); \
     } while (0)
     if (out_dtype == IM_DTYPE_F32) {
         if (vec) IM_UNPACK(float, true);
@@ -167,7 +171,7 @@ im_status im_act8_unpack(int32_t M, int32_t N, const im_act8 *in, const float *g
     }
 #undef IM_UNPACK
     g_launches.fetch_add(1, std::memory_order_relaxed);
-    return cudaGetLastError() == cudaSuccess ? IM_OK : IM_ERR_CUDA;
+    return e == cudaSuccess ? IM_OK : IM_ERR_CUDA;
 }
 
 }  // extern "C"

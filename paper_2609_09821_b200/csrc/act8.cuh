@@ -290,6 +290,14 @@ __device__ __forceinline__ void keep8(const Act8View &k, bool in, long long row,
     }
 }
 
+// For kernels launched programmatically: they may start while the kernel before them in the stream ends, and wait here for what that
+// writes; the kernel behind them may start in turn.
+__device__ __forceinline__ void after_previous_kernel()
+{
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+}
+
 inline bool aligned_to(const void *p, uintptr_t bytes) { return (reinterpret_cast<uintptr_t>(p) & (bytes - 1)) == 0; }
 inline size_t dtype_size(int dtype) { return dtype == IM_DTYPE_F32 ? 4 : 2; }
 inline bool float_dtype(int dtype) { return dtype == IM_DTYPE_F32 || dtype == IM_DTYPE_BF16; }

@@ -125,14 +125,14 @@ __device__ __forceinline__ uint32_t load_scales(const uint8_t *p, int blocks, bo
 {
     uint32_t w = 0u;
     if (word) {
-        asm volatile("ld.global.nc.b32 %0, [%1];" : "=r"(w) : "l"(p));
+        asm volatile("ld.global.b32 %0, [%1];" : "=r"(w) : "l"(p));
         return w;
     }
 #pragma unroll
     for (int i = 0; i < 4; ++i)
         if (i < blocks) {
             uint32_t b;
-            asm volatile("ld.global.nc.u8 %0, [%1];" : "=r"(b) : "l"(p + i));
+            asm volatile("ld.global.u8 %0, [%1];" : "=r"(b) : "l"(p + i));
             w |= b << (8 * i);
         }
     return w;
@@ -230,6 +230,8 @@ __device__ __forceinline__ void act8_tn_body(const CUtensorMap &map_a, const CUt
         if (leader_base != tmem_base) *abort_flag = 1;
     }
     if (PAIR) __syncthreads();
+
+    after_previous_kernel();                                 // nothing before this line touches global memory
 
     int stage = 0, acc = 0;
     uint32_t phase = 0, acc_phase = 0;
@@ -354,7 +356,7 @@ __device__ __forceinline__ void act8_tn_body(const CUtensorMap &map_a, const CUt
             if (MODE) {
 #pragma unroll
                 for (int c = 0; c < 4; ++c) {
-                    const auto at_col = [&](const float *p, int k, float other) { return p && k < P.No ? __ldg(p + k) : other; };
+                    const auto at_col = [&](const float *p, int k, float other) { return p && k < P.No ? p[k] : other; };
                     ga[c] = f2(at_col(P.gamma, col + 2 * c, 1.0f), at_col(P.gamma, col + 2 * c + 1, 1.0f));
                     be[c] = f2(at_col(P.beta, col + 2 * c, 0.0f), at_col(P.beta, col + 2 * c + 1, 0.0f));
                 }
@@ -441,7 +443,6 @@ __device__ __forceinline__ void act8_tn_body(const CUtensorMap &map_a, const CUt
             }
         }
     }
-    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");      // (the kernel that adds partial tiles waits for this one's end)
     // everyone meets (in a pair, so that shared memory and barriers outlive the peer's use of them); the allocating warp frees tensor memory
     if (*abort_flag && lane == 0) {
         // a wait ran out: copies and MMAs in flight get time to land (bounded)
@@ -478,7 +479,7 @@ constexpr int kSplitFrom = 12;             // slices
 template <int BLOCK_N, bool PAIR, bool SPLIT>
 __global__ void __launch_bounds__(256) act8_tn_finish_kernel(const Act8GemmParams P)
 {
-    asm volatile("griddepcontrol.wait;" ::: "memory");
+    after_previous_kernel();
     using PL = Plan<BLOCK_N, PAIR>;
     constexpr long long kSlot = (long long)BLOCK_N * PL::kCols;
     __shared__ float4 s_part[SPLIT ? 8 : 1][32];
@@ -569,10 +570,9 @@ cudaError_t launch_product(const Split &s, const CUtensorMap &map, const CUtenso
         return r;
     });
     if (e != cudaSuccess) return e;
-    if (s.pair) kpair<<<grid, kThreads, Plan<256, true>::kSmemBytes, st>>>(map, map_h, p);
-    else if (s.block_n == 64) k64<<<grid, kThreads, Plan<64, false>::kSmemBytes, st>>>(map, map_h, p);
-    else k128<<<grid, kThreads, Plan<128, false>::kSmemBytes, st>>>(map, map_h, p);
-    return cudaGetLastError();
+    if (s.pair) return launch_pdl(kpair, dim3(grid), dim3(kThreads), Plan<256, true>::kSmemBytes, st, 0, map, map_h, p);
+    if (s.block_n == 64) return launch_pdl(k64, dim3(grid), dim3(kThreads), Plan<64, false>::kSmemBytes, st, 0, map, map_h, p);
+    return launch_pdl(k128, dim3(grid), dim3(kThreads), Plan<128, false>::kSmemBytes, st, 0, map, map_h, p);
 }
 template <int FORM>
 cudaError_t launch_product(const Split &s, const CUtensorMap &map, const CUtensorMap &map_h, const Act8GemmParams &p, int mode, int grid, cudaStream_t st)

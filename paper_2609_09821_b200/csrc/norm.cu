@@ -46,13 +46,14 @@ __global__ void __launch_bounds__(kThreads) norm_forward_kernel(const NormForwar
     const auto first = [&](int c) { return VEC ? (c * T + t) * 8 : c * 8 * T + t; };
     constexpr int kStep = VEC ? 1 : T;                            // between a group's columns
     const float n = (float)N;
+    after_previous_kernel();
 
     for (int i = threadIdx.x; i < 8 * C * T; i += kThreads) {
         // element i of the layout: group c, half h, thread tt, position p of four
         const int p = i & 3, tt = (i >> 2) & (T - 1), h = (i >> 2) / T & 1, c = (i >> 2) / (2 * T);
         const int col = VEC ? (c * T + tt) * 8 + h * 4 + p : c * 8 * T + (h * 4 + p) * T + tt;
-        reinterpret_cast<float *>(s_affine)[i] = P.gamma && col < N ? __ldg(P.gamma + col) : 1.0f;
-        reinterpret_cast<float *>(s_affine)[8 * C * T + i] = P.beta && col < N ? __ldg(P.beta + col) : 0.0f;
+        reinterpret_cast<float *>(s_affine)[i] = P.gamma && col < N ? P.gamma[col] : 1.0f;
+        reinterpret_cast<float *>(s_affine)[8 * C * T + i] = P.beta && col < N ? P.beta[col] : 0.0f;
     }
     Eight<TX> raw[C];
     const auto load_row = [&](long long r) {
@@ -118,7 +119,7 @@ __global__ void __launch_bounds__(kThreads) norm_forward_kernel(const NormForwar
 constexpr int kFinishParts = 32;
 __global__ void __launch_bounds__(32 * kFinishParts) norm_finish_kernel(const float *partial, int n_partials, int N, float *dgamma, float *dbeta)
 {
-    asm volatile("griddepcontrol.wait;" ::: "memory");
+    after_previous_kernel();
     __shared__ double part[kFinishParts][33];
     const int c = blockIdx.x * 32 + threadIdx.x;                          // of [dgamma | dbeta]
     double s = 0.0;
@@ -155,8 +156,7 @@ cudaError_t launch_forward(const NormForward &a, int n_sm, cudaStream_t stream)
     });
     if (e != cudaSuccess) return e;
     const long long want = ((long long)a.M + kGroups - 1) / kGroups, most = (long long)n_sm * per_sm[dev].load();
-    kernel<<<(unsigned)(want < most ? want : most), kThreads, kSmem, stream>>>(a);
-    return cudaGetLastError();
+    return launch_pdl(kernel, dim3((unsigned)(want < most ? want : most)), dim3(kThreads), kSmem, stream, 0, a);
 }
 template <typename TX, typename TY>
 cudaError_t dispatch_forward(const NormForward &a, bool vec, int n_sm, cudaStream_t st)

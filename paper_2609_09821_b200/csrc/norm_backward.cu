@@ -64,6 +64,7 @@ __global__ void __launch_bounds__(cta_threads(T), 512 / cta_threads(T)) norm_bac
     const int t = threadIdx.x & (T - 1), g = threadIdx.x / T, N = P.N;
     const auto first = [&](int c) { return VEC ? (c * T + t) * 8 : c * 8 * T + t; };
     constexpr int kStep = VEC ? 1 : T;
+    after_previous_kernel();
     const TX *x = static_cast<const TX *>(P.x);
     TX *dx = static_cast<TX *>(P.dx);
     const TY *dy = static_cast<const TY *>(P.dy);
@@ -71,7 +72,7 @@ __global__ void __launch_bounds__(cta_threads(T), 512 / cta_threads(T)) norm_bac
 #pragma unroll
     for (int i = 0; i < E; ++i) {
         const int k = first(i >> 2) + 2 * (i & 3) * kStep;
-        const auto at = [&](const float *p, int c, float other) { return c >= N ? 0.0f : p ? __ldg(p + c) : other; };
+        const auto at = [&](const float *p, int c, float other) { return c >= N ? 0.0f : p ? p[c] : other; };
         ga[i] = f2(at(P.gamma, k, 1.0f), at(P.gamma, k + kStep, 1.0f));
         if (RELU) be[i] = f2(at(P.beta, k, 0.0f), at(P.beta, k + kStep, 0.0f));
         acc_g[i] = acc_b[i] = f2(0.0f);
@@ -219,7 +220,6 @@ __global__ void __launch_bounds__(cta_threads(T), 512 / cta_threads(T)) norm_bac
             }
         }
     }
-    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");      // (the kernel that adds the partial sums waits for this one's end)
     if (!P.partial) return;
     float *row = P.partial + (long long)blockIdx.x * 2 * N;
     if (kGroups > 1) {
@@ -266,9 +266,8 @@ cudaError_t launch_backward(const NormBackward &a, int n_sm, int *n_partials, cu
     long long most = (long long)n_sm * (512 / cta_threads(T));
     most = most < kNormMaxPartials ? most : kNormMaxPartials;
     const int grid = (int)(want < most ? want : most);
-    norm_backward_kernel<TX, TY, VEC, T, C, R, KEPT, RELU><<<grid, cta_threads(T), 0, stream>>>(a);
     *n_partials = grid;
-    return cudaGetLastError();
+    return launch_pdl(norm_backward_kernel<TX, TY, VEC, T, C, R, KEPT, RELU>, dim3((unsigned)grid), dim3(cta_threads(T)), 0, stream, 0, a);
 }
 template <typename TX, typename TY, bool KEPT, bool RELU>
 cudaError_t dispatch_width(const NormBackward &a, bool vec, int n_sm, int *n, cudaStream_t st)
