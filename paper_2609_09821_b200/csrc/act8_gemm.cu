@@ -38,6 +38,12 @@ constexpr int kFirstDecode = 2 + kScaleWarps, kFirstEpi = kFirstDecode + kDecode
 constexpr int kThreads = 32 * (kFirstEpi + kEpiWarps);
 constexpr int kMaxCtas = 160;              // (the workspace is sized for so many)
 constexpr int kChainBlocks = 20;           // k-blocks accumulated in tensor memory before they are added in fp32
+// Slots for codes and scales.  Even, so that a slot always belongs to the same one of the two groups of restoring warps: copies
+// complete in any order, and a group that waited for a slot's next phase while the one before, the other group's, was still
+// incomplete would take that one's parity for its own.  (The stages' `empty` barriers may change hands: MMAs complete in order, and a
+// group's wait for one follows its own wait for a later one of the round before.)
+constexpr int kRaw = 6;
+static_assert(kRaw % 2 == 0, "a slot belongs to one group");
 constexpr int kRawBytes = kBlockRows * kTileK, kScaleBytes = kBlockRows * (kTileK / kActBlock);
 constexpr int kMaxCols = 65536;            // of either operand
 constexpr int kMaxRows = 0x7fff0000;       // row numbers (a k-block beyond the last) in 32 bits
@@ -65,8 +71,8 @@ struct Plan {
     static constexpr int kStages = BLOCK_N == 64 ? 6 : 5;
     static constexpr int kAccs = PAIR ? 1 : 2;                                   // accumulators; behind them the sum of finished chains
     static constexpr int kTmemCols = BLOCK_N == 64 ? 256 : 512;                  // at least (kAccs + 1) BLOCK_N, a power of two
-    static constexpr size_t kSmemBytes = 1024 + (size_t)kStages * (kStageBytes + kRawBytes + kScaleBytes) + 512;
-    static_assert(kSmemBytes <= kSmemLimit && (4 * kStages + 2 * kAccs + 1) * 8 <= 512, "shared memory plan");
+    static constexpr size_t kSmemBytes = 1024 + (size_t)kStages * kStageBytes + (size_t)kRaw * (kRawBytes + kScaleBytes) + 512;
+    static_assert(kSmemBytes <= kSmemLimit && (2 * kStages + 2 * kRaw + 2 * kAccs + 1) * 8 <= 512, "shared memory plan");
 };
 
 // The k-blocks [k0, k0 + n) of a tile, one after another for a worker; slot: where their sum goes.
@@ -197,9 +203,9 @@ __device__ __forceinline__ void act8_tn_body(const CUtensorMap &map_a, const CUt
     using PL = Plan<BLOCK_N, PAIR>;
     extern __shared__ uint8_t smem_raw[];
     uint8_t *tiles = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
-    uint8_t *raw = tiles + (size_t)PL::kStages * PL::kStageBytes, *scales = raw + (size_t)PL::kStages * kRawBytes;
-    uint64_t *full = reinterpret_cast<uint64_t *>(scales + (size_t)PL::kStages * kScaleBytes);
-    uint64_t *empty = full + PL::kStages, *raw_full = empty + PL::kStages, *raw_empty = raw_full + PL::kStages, *acc_full = raw_empty + PL::kStages, *acc_empty = acc_full + PL::kAccs;
+    uint8_t *raw = tiles + (size_t)PL::kStages * PL::kStageBytes, *scales = raw + (size_t)kRaw * kRawBytes;
+    uint64_t *full = reinterpret_cast<uint64_t *>(scales + (size_t)kRaw * kScaleBytes);
+    uint64_t *empty = full + PL::kStages, *raw_full = empty + PL::kStages, *raw_empty = raw_full + kRaw, *acc_full = raw_empty + kRaw, *acc_empty = acc_full + PL::kAccs;
     uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(acc_empty + PL::kAccs);
     volatile int *abort_flag = reinterpret_cast<volatile int *>(tmem_slot + 1);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -209,7 +215,8 @@ __device__ __forceinline__ void act8_tn_body(const CUtensorMap &map_a, const CUt
 
     // full, acc_empty: of the pair's leader (rank 0), whose MMA warp waits on them; the others: each CTA's own
     if (threadIdx.x == 0) {
-        for (int s = 0; s < PL::kStages; ++s) { mbar_init(&full[s], 1 + kCtas * kGroupWarps); mbar_init(&empty[s], 1); mbar_init(&raw_full[s], 1 + kScaleWarps); mbar_init(&raw_empty[s], kGroupWarps); }
+        for (int s = 0; s < PL::kStages; ++s) { mbar_init(&full[s], 1 + kCtas * kGroupWarps); mbar_init(&empty[s], 1); }
+        for (int s = 0; s < kRaw; ++s) { mbar_init(&raw_full[s], 1 + kScaleWarps); mbar_init(&raw_empty[s], kGroupWarps); }
         for (int a = 0; a < PL::kAccs; ++a) { mbar_init(&acc_full[a], 1); mbar_init(&acc_empty[a], kCtas * kEpiWarps); }
         *abort_flag = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -306,6 +313,7 @@ __device__ __forceinline__ void act8_tn_body(const CUtensorMap &map_a, const CUt
         constexpr int kLead = 4;
         const bool one = warp == 2 && elect_one();
         const int r = (warp - 2) * 32 + lane;
+        int slot = 0;
         if (!g_skip_loads)
             for (int j = 0; ok && part_at(P, worker, j, part); ++j) {
                 const int col = (part.tile % P.tiles_k) * PL::kCols + (int)rank * kTileK, blocks = (P.No - col + kActBlock - 1) / kActBlock;
@@ -323,16 +331,16 @@ __device__ __forceinline__ void act8_tn_body(const CUtensorMap &map_a, const CUt
 #pragma unroll
                     for (int d = 0; d < kLead; ++d) {
                         if (i0 + d >= part.n) break;
-                        if (!(ok = warp_wait(smem_u32(&raw_empty[stage]), phase ^ 1u, abort_flag))) break;
+                        if (!(ok = warp_wait(smem_u32(&raw_empty[slot]), phase ^ 1u, abort_flag))) break;
                         if (one) {
-                            mbar_arrive_expect_tx(&raw_full[stage], kRawBytes);
-                            tma_load_2d(raw + (size_t)stage * kRawBytes, &map_h, &raw_full[stage], col, (part.k0 + i0 + d) * kBlockRows);
+                            mbar_arrive_expect_tx(&raw_full[slot], kRawBytes);
+                            tma_load_2d(raw + (size_t)slot * kRawBytes, &map_h, &raw_full[slot], col, (part.k0 + i0 + d) * kBlockRows);
                         }
-                        reinterpret_cast<uint32_t *>(scales + (size_t)stage * kScaleBytes)[r] = w[d];
+                        reinterpret_cast<uint32_t *>(scales + (size_t)slot * kScaleBytes)[r] = w[d];
                         __syncwarp();
-                        if (lane == 0) mbar_arrive(&raw_full[stage]);
+                        if (lane == 0) mbar_arrive(&raw_full[slot]);
                         ask(w[d]);
-                        if (++stage == PL::kStages) { stage = 0; phase ^= 1u; }
+                        if (++slot == kRaw) { slot = 0; phase ^= 1u; }
                     }
                 }
             }
@@ -348,7 +356,8 @@ __device__ __forceinline__ void act8_tn_body(const CUtensorMap &map_a, const CUt
         const uint32_t raw0 = smem_u32(raw) + (uint32_t)(r * 128) + (uint32_t)(((half * 4 + (cq >> 1)) ^ (r & 7)) << 4) + (uint32_t)((cq & 1) * 8);
         const uint32_t scale0 = smem_u32(scales) + (uint32_t)(r * 4 + half * 2 + (cq >> 2));
         const uint32_t full0 = PAIR ? map_to_rank(smem_u32(full), 0) : smem_u32(full), raw_full0 = smem_u32(raw_full), raw_empty0 = smem_u32(raw_empty), empty0 = smem_u32(empty);
-        int taken = 0;
+        int taken = 0, slot = group;
+        uint32_t raw_phase = 0;
         stage = group;
         for (int j = 0; ok && part_at(P, worker, j, part); ++j) {
             const int col = (part.tile % P.tiles_k) * PL::kCols + (int)rank * kTileK + half * 64 + cq * 8;
@@ -361,10 +370,10 @@ __device__ __forceinline__ void act8_tn_body(const CUtensorMap &map_a, const CUt
                     be[c] = f2(at_col(P.beta, col + 2 * c, 0.0f), at_col(P.beta, col + 2 * c + 1, 0.0f));
                 }
             }
-            // (taken: k-blocks of earlier parts; stage and phase: of this group's next one)
+            // (taken: k-blocks of earlier parts; slot, stage and their phases: of this group's next one)
             for (int i = (taken + group) & 1; i < part.n; i += 2) {
-                if (!(ok = warp_wait(raw_full0 + (uint32_t)(stage * 8), phase, abort_flag))) break;
-                const uint32_t from = raw0 + (uint32_t)(stage * kRawBytes), from_scale = scale0 + (uint32_t)(stage * kScaleBytes);
+                if (!(ok = warp_wait(raw_full0 + (uint32_t)(slot * 8), raw_phase, abort_flag))) break;
+                const uint32_t from = raw0 + (uint32_t)(slot * kRawBytes), from_scale = scale0 + (uint32_t)(slot * kScaleBytes);
                 uint2 w[4];
                 uint32_t byte[4];
 #pragma unroll
@@ -386,12 +395,14 @@ __device__ __forceinline__ void act8_tn_body(const CUtensorMap &map_a, const CUt
                 asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                 __syncwarp();
                 if (lane == 0) {
-                    mbar_arrive_addr(raw_empty0 + (uint32_t)(stage * 8));
+                    mbar_arrive_addr(raw_empty0 + (uint32_t)(slot * 8));
                     if (PAIR) mbar_arrive_remote(full0 + (uint32_t)(stage * 8));
                     else mbar_arrive_addr(full0 + (uint32_t)(stage * 8));
                 }
                 stage += 2;
                 if (stage >= PL::kStages) { stage -= PL::kStages; phase ^= 1u; }
+                slot += 2;
+                if (slot >= kRaw) { slot -= kRaw; raw_phase ^= 1u; }
             }
             taken += part.n;
         }

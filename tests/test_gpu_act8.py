@@ -195,6 +195,22 @@ def test_product_repeats_on_other_streams_and_in_graphs():
     assert all(torch.equal(C, o) for o in outs) and int(status) == 0
 
 
+@pytest.mark.parametrize("R,Mo,No,form", [(65536, 69, 512, ref.E4M3), (65536, 28, 512, ref.INT8), (16000, 512, 1024, ref.INT8)])
+def test_product_many_in_a_row(R, Mo, No, form):
+    # copies complete in another order each time; every launch gives the same bits
+    sets = [product(R, Mo, No, form, False, seed=s) for s in (1, 2, 3)]
+    wss = [B.gemm_act8_tn_workspace(R, Mo, No) for _ in sets]
+    outs = [torch.zeros(Mo, No, device="cuda") for _ in sets]
+    for i in range(600):
+        A, ck, _, _, _, C, status = sets[i % 3]
+        B.gemm_act8_tn(A, ck, outs[i % 3], wss[i % 3], status)
+        if i % 60 >= 57:
+            torch.cuda.synchronize()
+            assert torch.equal(outs[i % 3], C)
+            outs[i % 3].zero_()
+    assert all(int(s[-1]) == 0 for s in sets)
+
+
 def test_product_reports_a_wait_that_runs_out():
     R, Mo, No = 300, 64, 128
     A, ck, gamma, beta, relu, C, status = product(R, Mo, No, ref.INT8, False)
