@@ -693,38 +693,53 @@ def colsum(x, out, workspace, stream=None):
                                 workspace.numel() * workspace.element_size(), _st(stream)), "im_colsum_f32")
 
 
-# ---- layer norm and 8-bit activation checkpoints: 2-D CUDA tensors, float32 or bfloat16, row stride = stride(0)
+# ---- layer norm and 8-bit activation checkpoints: 2-D CUDA tensors, float32 or bfloat16, row stride = stride(0).
+# All tensors of a call lie on the current device.  These calls take a few microseconds on the GPU for small batches, so what they
+# check on the host is kept to a few attribute reads per tensor.
 ACT8_FORMS = {"int8": 0, "e4m3": 1}
+_torch = None
+_FLOATS = {}
 
 
-def _mat(t, what: str, rows: Optional[int] = None, cols: Optional[int] = None, dtypes=("float32", "bfloat16")):
-    """(pointer, row stride, dtype number) of a matrix on the current device, checked against the shape asked for."""
-    if t.dim() != 2 or not t.is_cuda or t.get_device() != _device() or str(t.dtype)[6:] not in dtypes:
-        raise ValueError("%s must be a matrix on the current CUDA device, %s" % (what, " or ".join(dtypes)))
-    m, n = t.shape
-    if (rows is not None and m != rows) or (cols is not None and n != cols) or (n > 1 and t.stride(1) != 1):
+def _here() -> int:
+    """The current CUDA device."""
+    global _torch
+    if _torch is None:
+        import torch
+        _torch = torch
+        _FLOATS.update({torch.float32: 0, torch.bfloat16: 1})
+    return _torch.cuda.current_device()
+
+
+def _on(stream, dev: int) -> int:
+    return (_torch.cuda.current_stream(dev) if stream is None else stream).cuda_stream
+
+
+def _mat(t, what: str, dev: int, rows=None, cols=None, types=_FLOATS):
+    """(pointer, row stride, dtype number) of a matrix on device dev, checked against the shape asked for."""
+    kind, shape = types.get(t.dtype), t.shape
+    if kind is None or len(shape) != 2 or t.get_device() != dev:
+        raise ValueError("%s must be a matrix on the current CUDA device, of one of the types %s" % (what, [str(k) for k in types]))
+    m, n = shape
+    ld, step = t.stride()
+    if (rows is not None and m != rows) or (cols is not None and n != cols) or (step != 1 and n > 1):
         raise ValueError("%s must be [%s, %s] with adjacent columns" % (what, m if rows is None else rows, n if cols is None else cols))
-    return t.data_ptr(), (t.stride(0) if m > 1 else max(n, 1)), int(t.dtype.itemsize == 2)
+    return t.data_ptr(), (ld if m > 1 else n), kind
 
 
-def _vec(t, n: int, what: str):
-    """Pointer of an optional contiguous float32 vector of n elements on the current device."""
+def _vec(t, n: int, what: str, dev: int):
+    """Pointer of an optional contiguous float32 vector of n elements on device dev."""
     if t is None:
         return None
-    if not t.is_cuda or t.get_device() != _device() or str(t.dtype) != "torch.float32" or t.numel() != n or not t.is_contiguous():
+    if t.dtype is not _torch.float32 or t.numel() != n or t.get_device() != dev or not t.is_contiguous():
         raise ValueError("%s must be a contiguous float32 vector of %d elements on the current CUDA device" % (what, n))
     return t.data_ptr()
 
 
-def _device() -> int:
-    import torch
-    return torch.cuda.current_device()
-
-
-def _scratch(t, what: str):
+def _scratch(t, what: str, dev: int):
     if t is None:
         return None, 0
-    if not t.is_cuda or t.get_device() != _device() or not t.is_contiguous():
+    if t.get_device() != dev or not t.is_contiguous():
         raise ValueError("%s must be a contiguous tensor on the current CUDA device" % what)
     return t.data_ptr(), t.numel() * t.element_size()
 
@@ -733,14 +748,13 @@ class Act8:
     """A [rows, cols] matrix in 8 bits (im_act8): code uint8 [rows, >= cols], scale uint8 [rows, >= ceil(cols / 32)]."""
 
     def __init__(self, code, scale, cols: int, form: str = "int8"):
-        rows = code.shape[0]
-        pc, lc, _ = _mat(code, "code", dtypes=("uint8",))
-        ps, ls, _ = _mat(scale, "scale", rows=rows, dtypes=("uint8",))
+        dev, rows = _here(), code.shape[0]
+        u8 = {_torch.uint8: 0}
+        pc, lc, _ = _mat(code, "code", dev, types=u8)
+        ps, ls, _ = _mat(scale, "scale", dev, rows, types=u8)
         if cols < 1 or code.shape[1] < cols or scale.shape[1] < -(-cols // 32):
             raise ValueError("code and scale are too narrow for %d columns" % cols)
-        if rows == 1:                       # (a lone row's stride is its width)
-            lc, ls = code.shape[1], scale.shape[1]
-        self.code, self.scale, self.rows, self.cols, self.form = code, scale, rows, cols, form
+        self.code, self.scale, self.rows, self.cols, self.form, self.device = code, scale, rows, cols, form, dev
         self.view = Act8View(pc, lc, ps, ls, ACT8_FORMS[form])
         self.ref = C.byref(self.view)
 
@@ -749,13 +763,13 @@ class Act8:
         """Storage for `rows` rows on the current device, laid out as gemm_act8_tn reads it (rows of a multiple of 16 codes)."""
         import torch
         new = lambda n: torch.zeros(rows, n, dtype=torch.uint8, device="cuda")  # noqa: E731
-        return cls(new(-(-cols // 16) * 16), new(-(-cols // 32)), cols, form)
+        return cls(new(-(-cols // 16) * 16), new(-(-cols // 128) * 4), cols, form)
 
 
-def _kept(ckpt, rows: int, cols: int):
+def _kept(ckpt, rows: int, cols: int, dev: int):
     if ckpt is None:
         return None
-    if ckpt.rows != rows or ckpt.cols != cols or ckpt.code.get_device() != _device():
+    if ckpt.rows != rows or ckpt.cols != cols or ckpt.device != dev:
         raise ValueError("the checkpoint must be [%d, %d], on the current CUDA device" % (rows, cols))
     return ckpt.ref
 
@@ -763,11 +777,12 @@ def _kept(ckpt, rows: int, cols: int):
 def layer_norm(x, gamma, beta, y, mean=None, rstd=None, eps: float = 1e-5, relu: bool = False, ckpt: Optional[Act8] = None, stream=None):
     """y [M, N] = act(gamma xh + beta), xh the rows of x [M, N] brought to mean 0 and variance 1; the row statistics into
     mean, rstd [M] and xh in 8 bits into ckpt, where given.  gamma, beta [N] or None; y may be x."""
+    dev = _here()
     M, N = x.shape
-    px, lx, dx = _mat(x, "x")
-    py, ly, dy = _mat(y, "y", M, N)
-    _check(load().im_layer_norm_forward(M, N, px, lx, dx, _vec(gamma, N, "gamma"), _vec(beta, N, "beta"), eps, int(relu), py, ly, dy,
-                                        _vec(mean, M, "mean"), _vec(rstd, M, "rstd"), _kept(ckpt, M, N), _st(stream)),
+    px, lx, dx = _mat(x, "x", dev)
+    py, ly, dy = _mat(y, "y", dev, M, N)
+    _check(load().im_layer_norm_forward(M, N, px, lx, dx, _vec(gamma, N, "gamma", dev), _vec(beta, N, "beta", dev), eps, relu, py, ly, dy,
+                                        _vec(mean, M, "mean", dev), _vec(rstd, M, "rstd", dev), _kept(ckpt, M, N, dev), _on(stream, dev)),
            "im_layer_norm_forward")
 
 
@@ -780,38 +795,39 @@ def layer_norm_workspace(M: int, N: int):
 def layer_norm_backward(dy, gamma, beta, rstd, dx, dgamma, dbeta, workspace, relu: bool = False, x=None, mean=None,
                         ckpt: Optional[Act8] = None, stream=None):
     """dx [M, N], dgamma, dbeta [N] from dy [M, N], the gradient at layer_norm's y: with x and mean as that call had them, or
-    with its ckpt instead of both.  Any of dx, dgamma and dbeta may be None; dx (float32 if None) has x's type."""
+    with its ckpt instead of both.  Any of dx, dgamma and dbeta may be None; dx has x's type (with ckpt: either)."""
+    dev = _here()
     M, N = dy.shape
-    pdy, ldy, ddy = _mat(dy, "dy")
-    px = lx = pdx = ldx = None
-    xt = 0
-    if x is not None:
-        px, lx, xt = _mat(x, "x", M, N)
+    pdy, ldy, ddy = _mat(dy, "dy", dev)
+    px, lx, xt = (None, 0, 0) if x is None else _mat(x, "x", dev, M, N)
+    pdx, ldx = None, 0
     if dx is not None:
-        pdx, ldx, dt = _mat(dx, "dx", M, N)
+        pdx, ldx, dt = _mat(dx, "dx", dev, M, N)
         if x is not None and dt != xt:
             raise ValueError("dx must have x's dtype")
         xt = dt
-    pw, nw = _scratch(workspace, "workspace")
-    _check(load().im_layer_norm_backward(M, N, pdy, ldy, ddy, px, lx or 0, xt, _vec(mean, M, "mean"), _vec(rstd, M, "rstd"),
-                                         _kept(ckpt, M, N), _vec(gamma, N, "gamma"), _vec(beta, N, "beta"), int(relu), pdx, ldx or 0,
-                                         _vec(dgamma, N, "dgamma"), _vec(dbeta, N, "dbeta"), pw, nw, _st(stream)),
+    pw, nw = _scratch(workspace, "workspace", dev)
+    _check(load().im_layer_norm_backward(M, N, pdy, ldy, ddy, px, lx, xt, _vec(mean, M, "mean", dev), _vec(rstd, M, "rstd", dev),
+                                         _kept(ckpt, M, N, dev), _vec(gamma, N, "gamma", dev), _vec(beta, N, "beta", dev), relu, pdx, ldx,
+                                         _vec(dgamma, N, "dgamma", dev), _vec(dbeta, N, "dbeta", dev), pw, nw, _on(stream, dev)),
            "im_layer_norm_backward")
 
 
 def act8_pack(x, ckpt: Act8, stream=None):
     """The matrix x in 8 bits."""
+    dev = _here()
     M, N = x.shape
-    px, lx, dt = _mat(x, "x")
-    _check(load().im_act8_pack(M, N, px, lx, dt, _kept(ckpt, M, N), _st(stream)), "im_act8_pack")
+    px, lx, dt = _mat(x, "x", dev)
+    _check(load().im_act8_pack(M, N, px, lx, dt, _kept(ckpt, M, N, dev), _on(stream, dev)), "im_act8_pack")
 
 
 def act8_unpack(ckpt: Act8, out, gamma=None, beta=None, relu: bool = False, stream=None):
     """out = the values ckpt stands for, or act(gamma v + beta) of them."""
+    dev = _here()
     M, N = out.shape
-    po, lo, dt = _mat(out, "out")
-    _check(load().im_act8_unpack(M, N, _kept(ckpt, M, N), _vec(gamma, N, "gamma"), _vec(beta, N, "beta"), int(relu), po, lo, dt, _st(stream)),
-           "im_act8_unpack")
+    po, lo, dt = _mat(out, "out", dev)
+    _check(load().im_act8_unpack(M, N, _kept(ckpt, M, N, dev), _vec(gamma, N, "gamma", dev), _vec(beta, N, "beta", dev), relu, po, lo, dt,
+                                 _on(stream, dev)), "im_act8_unpack")
 
 
 def gemm_act8_tn_workspace(R: int, Mo: int, No: int):
@@ -822,16 +838,21 @@ def gemm_act8_tn_workspace(R: int, Mo: int, No: int):
 
 def gemm_act8_tn(A, ckpt: Act8, Cout, workspace, status, gamma=None, beta=None, relu: bool = False, stream=None):
     """Cout [Mo, No] (float32) = A [R, Mo] (bfloat16) transposed times the matrix ckpt [R, No] stands for (act8_unpack's
-    bfloat16 values under gamma, beta, relu)."""
+    bfloat16 values under gamma, beta, relu).  status: one int32 on the device."""
+    dev = _here()
     R, Mo = A.shape
     No = ckpt.cols
-    pa, la, _ = _mat(A, "A", dtypes=("bfloat16",))
+    pa, la, kind = _mat(A, "A", dev)
+    pc, lc, ck = _mat(Cout, "Cout", dev, Mo, No)
+    if kind != 1 or ck != 0:
+        raise ValueError("A must be bfloat16 and Cout float32")
     if R == 1:
         la = -(-Mo // 8) * 8                # (a lone row's stride is free)
-    pc, lc, _ = _mat(Cout, "Cout", Mo, No, dtypes=("float32",))
-    pw, nw = _scratch(workspace, "workspace")
-    _check(load().im_gemm_act8_tn(pa, la, _kept(ckpt, R, No), pc, lc, R, Mo, No, _vec(gamma, No, "gamma"), _vec(beta, No, "beta"),
-                                  int(relu), pw, nw, _ptr(status), _st(stream)), "im_gemm_act8_tn")
+    pw, nw = _scratch(workspace, "workspace", dev)
+    if status.get_device() != dev or status.element_size() != 4:
+        raise ValueError("status must be an int32 on the current CUDA device")
+    _check(load().im_gemm_act8_tn(pa, la, _kept(ckpt, R, No, dev), pc, lc, R, Mo, No, _vec(gamma, No, "gamma", dev), _vec(beta, No, "beta", dev),
+                                  relu, pw, nw, status.data_ptr(), _on(stream, dev)), "im_gemm_act8_tn")
 
 
 class _DeviceArray:
