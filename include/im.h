@@ -565,7 +565,7 @@ im_status im_colsum_f32(const float *x, int64_t ld, int64_t rows, int32_t cols, 
  * im_act8: a matrix in 8 bits.  Columns 32 b .. 32 b + 31 of a row (fewer at its end) share a power of two 2^e, the least
  * with e >= -100 for which the largest magnitude among them is at most 127 2^e (IM_ACT8_INT8) or 448 2^e (IM_ACT8_E4M3); a code is
  * value / 2^e rounded to nearest, ties to even, as int8 or as e4m3 (no infinities, 448 the largest).  The scale byte is e + 127;
- * 255 marks a block with an infinity or a NaN in it: its codes are 0 and every value of it is restored as NaN.
+ * 255 marks a block with an infinity or a NaN in it: its codes are 0, and code times an infinite scale restores NaN.
  *   code   DEVICE [rows][ld_code] bytes      scale  DEVICE [rows][ld_scale] bytes, ld_scale >= ceil(N / 32)
  * The struct is HOST memory and not kept.  A restored value, code 2^e, is exact in bf16 (what rounded up to
  * 2^128 or more is restored as an infinity).
@@ -577,7 +577,8 @@ im_status im_colsum_f32(const float *x, int64_t ld, int64_t rows, int32_t cols, 
  * im_layer_norm_backward: dy [M][N] the gradient at y.  With h = dy where relu == 0 or fl32(gamma xh + beta) > 0, else 0:
  *   dx = rstd (gamma h - mean_n(gamma h) - xh mean_n(gamma h xh)),  dgamma = sum_rows h xh,  dbeta = sum_rows h.
  *   xh comes from x and mean (then it is the forward's, bit for bit, and so is the ReLU's decision) or, with x == NULL, from
- *   `kept`; exactly one of the two is given.  rstd in either case.  x_dtype: of x and dx.  dx may be dy or x (same type and
+ *   `kept` (then a pre-activation nearer to 0 than half a step of its block may be decided otherwise than by the forward
+ *   pass); exactly one of the two is given.  rstd in either case.  x_dtype: of x and dx.  dx may be dy or x (same type and
  *   stride) or NULL;  dgamma, dbeta DEVICE float [N], either NULL (not all three).  workspace: DEVICE, 16-byte
  *   aligned, at least im_layer_norm_workspace_bytes(M, N) (needed for dgamma or dbeta; contents irrelevant; calls that may
  *   overlap on the GPU need one each).

@@ -82,7 +82,8 @@ __device__ __forceinline__ uint32_t act8_scale_byte(uint32_t amax, int form)
     int b = (int)(amax >> 23) - (i8 ? 6 : 8) + ((amax & 0x7fffffu) > (i8 ? 0x7e0000u : 0x600000u) ? 1 : 0);
     return (uint32_t)(b < 27 ? 27 : b);
 }
-__device__ __forceinline__ float act8_scale(uint32_t byte) { return __uint_as_float(byte == 255u ? 0x7fc00000u : byte << 23); }
+// 2^e; infinite for a marked block (255), whose codes are 0: NaN
+__device__ __forceinline__ float act8_scale(uint32_t byte) { return __uint_as_float(byte << 23); }
 // 1 / 2^e, for byte != 255
 __device__ __forceinline__ float act8_inverse(uint32_t byte) { return __uint_as_float((254u - byte) << 23); }
 

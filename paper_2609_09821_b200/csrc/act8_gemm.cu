@@ -387,8 +387,7 @@ __device__ __forceinline__ void act8_tn_body(const CUtensorMap &map_a, const CUt
 #pragma unroll
                 for (int q = 0; q < 4; ++q) {
                     uint32_t o[4];
-                    // (a marked block's byte, 255, is an infinity here, and its codes are 0: NaN)
-                    restore8<FORM, MODE>(w[q], __uint_as_float(byte[q] << 23), ga, be, o);
+                    restore8<FORM, MODE>(w[q], act8_scale(byte[q]), ga, be, o);
                     if (MODE && rows_left < kBlockRows && r + 16 * q >= rows_left) o[0] = o[1] = o[2] = o[3] = 0u;   // behind the last row: zeros, not beta
                     asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(to + q * 2048), "r"(o[0]), "r"(o[1]), "r"(o[2]), "r"(o[3]) : "memory");
                 }

@@ -141,6 +141,23 @@ def test_backward_against_differences_of_the_forward():
         assert abs(float((grad.double() * d).sum()) - want) <= 2e-6 * (1 + float((grad.double().abs() * d.abs()).sum()))
 
 
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+def test_the_backward_pass_opens_the_elements_that_the_forward_left_positive(dtype):
+    # one row: dbeta is dy where y > 0; half of the pre-activations lie within a few roundings of 0
+    N = 4096
+    g = torch.Generator("cuda").manual_seed(11)
+    for _ in range(20):
+        x = torch.randn(1, N, device="cuda", generator=g).to(getattr(torch, dtype))
+        gamma, beta = torch.rand(N, device="cuda", generator=g) + 0.5, torch.randn(N, device="cuda", generator=g)
+        xh, mean, rstd = torch.empty(1, N, device="cuda"), torch.empty(1, device="cuda"), torch.empty(1, device="cuda")
+        B.layer_norm(x, None, None, xh, mean, rstd)
+        beta[::2] = -(gamma * xh[0])[::2]
+        y, db, dy = torch.empty(1, N, device="cuda"), torch.empty(N, device="cuda"), torch.randn(1, N, device="cuda", generator=g)
+        B.layer_norm(x, gamma, beta, y, relu=True)
+        B.layer_norm_backward(dy, gamma, beta, rstd, None, None, db, B.layer_norm_workspace(1, N), relu=True, x=x, mean=mean)
+        assert torch.equal(db, torch.where(y[0] > 0, dy[0], torch.zeros(N, device="cuda")))
+
+
 def test_outputs_may_be_left_out_and_lie_on_inputs():
     M, N = 133, 1024
     g = torch.Generator("cuda").manual_seed(8)
