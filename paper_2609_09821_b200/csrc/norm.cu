@@ -16,17 +16,18 @@ namespace {
 
 constexpr int kThreads = 256;
 
+// The sum of v over the T threads of a row; more than a warp's meet at the row group's own barrier.
 template <int T>
-__device__ __forceinline__ float row_sum(float v, float *shared)
+__device__ __forceinline__ float row_sum(float v, float *shared, int group)
 {
 #pragma unroll
     for (int o = (T < 32 ? T : 32) / 2; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
     if (T > 32) {
         if ((threadIdx.x & 31) == 0) shared[threadIdx.x >> 5] = v;
-        __syncthreads();
+        asm volatile("bar.sync %0, %1;" ::"r"(1 + group), "n"(T) : "memory");
         v = 0.0f;
 #pragma unroll
-        for (int w = 0; w < T / 32; ++w) v += shared[w];
+        for (int w = 0; w < T / 32; ++w) v += shared[group * (T / 32) + w];
     }
     return v;
 }
@@ -72,7 +73,7 @@ __global__ void __launch_bounds__(kThreads) norm_forward_kernel(const NormForwar
         F2 s = v[0];
 #pragma unroll
         for (int i = 1; i < 4 * C; ++i) s = add2(s, v[i]);
-        const float mean = row_sum<T>(lo(s) + hi(s), s_sum[0]) / n;
+        const float mean = row_sum<T>(lo(s) + hi(s), s_sum[0], g) / n;
         const F2 minus = f2(-mean);
         s = f2(0.0f);
 #pragma unroll
@@ -87,7 +88,7 @@ __global__ void __launch_bounds__(kThreads) norm_forward_kernel(const NormForwar
 #pragma unroll
             for (int i = 0; i < 4; ++i) s = fma2(v[4 * c + i], v[4 * c + i], s);
         }
-        const float rstd = 1.0f / sqrtf(row_sum<T>(lo(s) + hi(s), s_sum[1]) / n + P.eps);
+        const float rstd = 1.0f / sqrtf(row_sum<T>(lo(s) + hi(s), s_sum[1], g) / n + P.eps);
         if (r < P.M && t == 0) {
             if (P.mean) P.mean[r] = mean;
             if (P.rstd) P.rstd[r] = rstd;
@@ -175,8 +176,8 @@ cudaError_t dispatch_forward(const NormForward &a, bool vec, int n_sm, cudaStrea
     if (N <= 512) return launch_forward<TX, TY, true, 32, 2>(a, n_sm, st);
     if (N <= 768) return launch_forward<TX, TY, true, 32, 3>(a, n_sm, st);
     if (N <= 1024) return launch_forward<TX, TY, true, 32, 4>(a, n_sm, st);
-    if (N <= 2048) return launch_forward<TX, TY, true, 256, 1>(a, n_sm, st);
-    if (N <= 4096) return launch_forward<TX, TY, true, 256, 2>(a, n_sm, st);
+    if (N <= 2048) return launch_forward<TX, TY, true, 64, 4>(a, n_sm, st);
+    if (N <= 4096) return launch_forward<TX, TY, true, 128, 4>(a, n_sm, st);
     return launch_forward<TX, TY, true, 256, 4>(a, n_sm, st);
 }
 
