@@ -260,6 +260,17 @@ __device__ __forceinline__ void store_codes8(uint8_t *row, int col, int step, in
     }
 }
 
+// Scale byte and codes of eight neighbouring values, given the largest magnitude of their block.  in: the row exists.
+template <bool ALIGNED>
+__device__ __forceinline__ void keep_side8(const Act8View &k, bool in, long long row, int col, int cols, const F2 *v, uint32_t amax)
+{
+    const uint32_t byte = act8_scale_byte(amax, k.form);
+    const uint2 w = act8_encode8(v, byte, k.form);
+    if (!in || col >= cols) return;
+    if ((col & 31) == 0) k.scale[row * k.ld_scale + (col >> 5)] = (uint8_t)byte;
+    store_codes8<ALIGNED>(k.code + row * k.ld_code, col, 1, cols, w);
+}
+
 // Scale byte and codes of a thread's eight values of a row.  SIDE: they are neighbours, and four threads in a row make a block; else
 // they lie T columns apart, and a block is one value of each lane.  ALIGNED: eight codes may be stored at once (SIDE only).
 // Whole warps; in: the row exists.
@@ -271,11 +282,7 @@ __device__ __forceinline__ void keep8(const Act8View &k, bool in, long long row,
         uint32_t amax = abs_bits_max8(v);
         amax = max(amax, __shfl_xor_sync(0xffffffffu, amax, 1));
         amax = max(amax, __shfl_xor_sync(0xffffffffu, amax, 2));
-        const uint32_t byte = act8_scale_byte(amax, k.form);
-        const uint2 w = act8_encode8(v, byte, k.form);
-        if (!in || col >= cols) return;
-        if ((col & 31) == 0) k.scale[row * k.ld_scale + (col >> 5)] = (uint8_t)byte;
-        store_codes8<ALIGNED>(k.code + row * k.ld_code, col, 1, cols, w);
+        keep_side8<ALIGNED>(k, in, row, col, cols, v, amax);
     } else {
         uint32_t w[2] = {0u, 0u};
 #pragma unroll

@@ -95,12 +95,28 @@ __global__ void __launch_bounds__(kThreads) norm_forward_kernel(const NormForwar
         }
         const F2 scale = f2(rstd);
 #pragma unroll
+        for (int i = 0; i < 4 * C; ++i) v[i] = mul2(v[i], scale);      // xh, by the operations that the backward pass repeats
+        if (P.keep.code) {
+            if (VEC) {
+                // (step by step over all groups: the exchanges of one hide under those of the others)
+                uint32_t amax[C];
+#pragma unroll
+                for (int c = 0; c < C; ++c) amax[c] = abs_bits_max8(v + 4 * c);
+#pragma unroll
+                for (int c = 0; c < C; ++c) amax[c] = max(amax[c], __shfl_xor_sync(0xffffffffu, amax[c], 1));
+#pragma unroll
+                for (int c = 0; c < C; ++c) amax[c] = max(amax[c], __shfl_xor_sync(0xffffffffu, amax[c], 2));
+#pragma unroll
+                for (int c = 0; c < C; ++c) keep_side8<true>(P.keep, r < P.M, r, first(c), N, v + 4 * c, amax[c]);
+            } else {
+#pragma unroll
+                for (int c = 0; c < C; ++c) keep8<false, false, T>(P.keep, r < P.M, r, first(c), N, v + 4 * c);
+            }
+        }
+#pragma unroll
         for (int c = 0; c < C; ++c) {
             const int col = first(c);
             F2 *e = v + 4 * c;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) e[i] = mul2(e[i], scale);      // xh, by the operations that the backward pass repeats
-            if (P.keep.code) keep8<VEC, VEC, T>(P.keep, r < P.M, r, col, N, e);
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
                 const float4 ga = s_affine[(2 * c + h) * T + t], be = s_affine[(2 * (C + c) + h) * T + t];
