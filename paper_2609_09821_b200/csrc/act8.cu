@@ -12,7 +12,8 @@ constexpr int kStride = 32;                // columns between a thread's eight v
 // A CTA covers 2^tx_bits groups of eight columns by the other threads' rows.  VEC: a thread's eight columns are neighbours, and a block
 // of 32 columns is four neighbouring threads; else (tx_bits 5) they lie 32 apart, a block is a warp, and a warp's accesses to single
 // elements are side by side (a row of eight neighbours a thread by single stores: 19 us for 9001 x 361 in place of 4).
-// Both kernels do a few operations per byte: what bounds them is HBM, hence 16-byte loads and several rows in flight per thread.
+// Both kernels do a few operations per byte: what bounds them is HBM, hence 16-byte loads and several rows in flight per thread
+// (131072 x 1024 bf16 to int8 80 us, back 67: 5.1 and 6.0 TB/s).
 template <typename T, bool VEC>
 __global__ void __launch_bounds__(kThreads, 4) pack_kernel(const T *x, long long ldx, int M, int N, const Act8View out, int tx_bits)
 {

@@ -16,6 +16,10 @@
 // after kChainBlocks k-blocks the epilogue adds the accumulator to the part's sum, which lies in tensor memory too, and the next chain
 // starts from zero.
 //
+// 131072 x 1024 x 1024 from int8 under gamma, beta and ReLU: 236 us, 1160 TFLOP/s (in a long run, at the power limit, 293);
+// 16000 x 512 x 1024 29 us, of which 12 are products; 65536 x 69 x 512 22 us.  What bounds the large product is the restoring warps,
+// which take two thirds of the issue slots, and the stop at each chain's end.
+//
 // Work is cut along the rows where there are fewer output tiles than SMs.  Each tile's rows are shared out to `slices`
 // workers (a CTA or a pair) in equal ranges, so that workers of different tiles walk the same rows at the same time and share
 // them in L2; workers left over take the last rows of all tiles, in a row.  Partial tiles go to the workspace and a second
@@ -37,7 +41,8 @@ constexpr int kScaleWarps = 2, kDecodeWarps = 16, kGroupWarps = 8, kEpiWarps = 8
 constexpr int kFirstDecode = 2 + kScaleWarps, kFirstEpi = kFirstDecode + kDecodeWarps;
 constexpr int kThreads = 32 * (kFirstEpi + kEpiWarps);
 constexpr int kMaxCtas = 160;              // (the workspace is sized for so many)
-constexpr int kChainBlocks = 20;           // k-blocks accumulated in tensor memory before they are added in fp32
+constexpr int kChainBlocks = 20;           // k-blocks accumulated in tensor memory before they are added in fp32: the error of a
+                                           // product is 6e-7 (2-norm) with 16, 9e-7 with 20, 1.3e-6 with 28
 // Slots for codes and scales.  Even, so that a slot always belongs to the same one of the two groups of restoring warps: copies
 // complete in any order, and a group that waited for a slot's next phase while the one before, the other group's, was still
 // incomplete would take that one's parity for its own.  (The stages' `empty` barriers may change hands: MMAs complete in order, and a
