@@ -35,6 +35,7 @@
 #ifndef IM_H_
 #define IM_H_
 
+#include <stddef.h>
 #include <stdint.h>
 
 #ifdef __cplusplus

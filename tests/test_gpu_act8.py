@@ -226,3 +226,21 @@ def test_product_reports_a_wait_that_runs_out():
     C2 = torch.empty(Mo, No, device="cuda")
     B.gemm_act8_tn(A, ck, C2, ws, status)
     assert torch.equal(C2, C[:, :No]) and int(status) == 0
+
+
+def test_beyond_32_bits_of_elements():
+    rows, cols, Mo = 2 ** 20 + 3, 4096 + 16, 64
+    x = torch.zeros(rows, cols, device="cuda", dtype=torch.bfloat16)
+    x[-1] = (torch.arange(cols, device="cuda") % 127).bfloat16()
+    ck = B.Act8.empty(rows, cols)
+    B.act8_pack(x, ck)
+    want = ref.kept(x[-1:], ref.INT8)
+    assert int(torch.count_nonzero(ck.code[:-1])) == 0
+    x.fill_(1.0)
+    B.act8_unpack(ck, x)
+    assert torch.equal(x[-1:].double(), want) and bool((x[:-1].view(torch.int16) == 0).all())
+    A = torch.zeros(rows, Mo, device="cuda", dtype=torch.bfloat16)
+    A[-1] = torch.randn(Mo, device="cuda").bfloat16()
+    C, status = torch.empty(Mo, cols, device="cuda"), torch.zeros(1, dtype=torch.int32, device="cuda")
+    B.gemm_act8_tn(A, ck, C, B.gemm_act8_tn_workspace(rows, Mo, cols), status)
+    assert torch.equal(C.double(), A[-1].double()[:, None] * want) and int(status) == 0      # one product a sum: exact

@@ -281,3 +281,51 @@ def test_rows_beyond_32_bits_of_elements():
     torch.cuda.synchronize()
     check_forward(want, None, None, x[-1:], mean[-1:], rstd[-1:], False)
     assert bool((x[:-1].view(torch.int16) == 0).all())
+
+
+def test_backward_beyond_32_bits_of_elements():
+    M, N = 2 ** 20 + 3, 4096 + 8
+    dy = torch.zeros(M, N, device="cuda", dtype=torch.bfloat16)
+    dy[-1] = (torch.arange(N, device="cuda") % 13).bfloat16()
+    ck = B.Act8.empty(M, N)
+    ck.scale.fill_(120)
+    ck.code[-1, :N] = torch.arange(N, device="cuda").remainder(251).to(torch.uint8)
+    rstd = torch.ones(M, device="cuda")
+    dg, db = torch.empty(N, device="cuda"), torch.empty(N, device="cuda")
+    h = dy[-1:].double()
+    xh = ck.code[-1:, :N].view(torch.int8).double() * 2.0 ** (120 - 127)
+    B.layer_norm_backward(dy, None, None, rstd, dy, dg, db, B.layer_norm_workspace(M, N), ckpt=ck)
+    rdx, rg, rb, err, _, _ = ref.backward(h, xh, None, rstd[-1:], None, False)
+    assert torch.equal(dg.double(), (h * xh)[0]) and torch.equal(db.double(), h[0])       # one row: exact products
+    assert bool(((dy[-1:].double() - rdx).abs() <= err + (rdx.abs() + err) * ref.HALF[torch.bfloat16]).all())
+    assert bool((dy[:-1].view(torch.int16) == 0).all())
+
+
+def test_tensors_that_do_not_fit_are_refused():
+    M, N = 8, 64
+    x, y, v = torch.zeros(M, N, device="cuda"), torch.zeros(M, N, device="cuda"), torch.zeros(N, device="cuda")
+    ck = B.Act8.empty(M, N)
+    for bad in (x.cpu(), x.half(), x.double(), x.t(), x[:, :32], x[:4], x.view(-1)):
+        with pytest.raises(ValueError):
+            B.layer_norm(x, v, v, bad)
+        with pytest.raises(ValueError):
+            B.act8_unpack(B.Act8.empty(M, N), bad)
+    for bad in (v.cpu(), v.bfloat16(), v[:32], torch.zeros(2 * N, device="cuda")[::2]):
+        with pytest.raises(ValueError):
+            B.layer_norm(x, bad, None, y)
+        with pytest.raises(ValueError):
+            B.layer_norm_backward(x, bad, None, torch.ones(M, device="cuda"), y, None, None, None, x=x, mean=torch.zeros(M, device="cuda"))
+    with pytest.raises(ValueError):
+        B.layer_norm(x, v, v, y, ckpt=B.Act8.empty(M, 32))
+    with pytest.raises(ValueError):
+        B.Act8(ck.code[:, :32], ck.scale, N)
+    with pytest.raises(ValueError):
+        B.Act8(ck.code, ck.scale[:4], N)
+    with pytest.raises(KeyError):
+        B.Act8(ck.code, ck.scale, N, "int4")
+    with pytest.raises(ValueError):
+        B.gemm_act8_tn(x, ck, torch.empty(N, N, device="cuda"), None, torch.zeros(1, dtype=torch.int32, device="cuda"))      # A not bf16
+    with pytest.raises(B.ImError):
+        B.layer_norm(torch.zeros(2, 8200, device="cuda"), None, None, torch.zeros(2, 8200, device="cuda"))
+    with pytest.raises(B.ImError):
+        B.layer_norm(torch.zeros(0, 8, device="cuda"), None, None, torch.zeros(0, 8, device="cuda"))
