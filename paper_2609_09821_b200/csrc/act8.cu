@@ -13,7 +13,7 @@ constexpr int kStride = 32;                // columns between a thread's eight v
 // of 32 columns is four neighbouring threads; else (tx_bits 5) they lie 32 apart, a block is a warp, and a warp's accesses to single
 // elements are side by side (a row of eight neighbours a thread by single stores: 19 us for 9001 x 361 in place of 4).
 // Both kernels do a few operations per byte: what bounds them is HBM, hence 16-byte loads and several rows in flight per thread
-// (131072 x 1024 bf16 to int8 80 us, back 67: 5.1 and 6.0 TB/s).
+// (131072 x 1024 bf16 to int8 75 us, back 69: 5.4 and 5.9 TB/s; the maxima row by row: 78 us).
 template <typename T, bool VEC>
 __global__ void __launch_bounds__(kThreads, 4) pack_kernel(const T *x, long long ldx, int M, int N, const Act8View out, int tx_bits)
 {
@@ -30,12 +30,23 @@ __global__ void __launch_bounds__(kThreads, 4) pack_kernel(const T *x, long long
             const long long r = min(r0 + ty + i * row_step, (long long)M - 1);
             raw[i] = load8<VEC>(x + r * ldx, col, kStride, N);
         }
+        uint32_t amax[kRows];
+        if (VEC) {
+            // (step by step over all rows: the exchanges of one hide under those of the others)
+#pragma unroll
+            for (int i = 0; i < kRows; ++i) amax[i] = largest8(raw[i]);
+#pragma unroll
+            for (int i = 0; i < kRows; ++i) amax[i] = max(amax[i], __shfl_xor_sync(0xffffffffu, amax[i], 1));
+#pragma unroll
+            for (int i = 0; i < kRows; ++i) amax[i] = max(amax[i], __shfl_xor_sync(0xffffffffu, amax[i], 2));
+        }
 #pragma unroll
         for (int i = 0; i < kRows; ++i) {
             const long long r = r0 + ty + i * row_step;
             F2 v[4];
             unpack8(raw[i], v);
-            keep8<VEC, VEC, kStride>(out, r < M, r, col, N, v);
+            if (VEC) keep_side8(out, r < M, r, col, N, v, amax[i]);
+            else keep8<kStride>(out, r < M, r, col, N, v);
         }
     }
 }

@@ -233,6 +233,19 @@ __device__ __forceinline__ void store8(T *row, int col, int step, int cols, cons
         if (c < cols) store_as(row + c, floored<RELU>(j & 1 ? hi(v[j >> 1]) : lo(v[j >> 1])));
     }
 }
+// The largest magnitude among a thread's eight values, as fp32 bits (bf16: two at a time, by their own bits).
+__device__ __forceinline__ uint32_t largest8(const Eight<float> &e)
+{
+    F2 v[4];
+    unpack8(e, v);
+    return abs_bits_max8(v);
+}
+__device__ __forceinline__ uint32_t largest8(const Eight<__nv_bfloat16> &e)
+{
+    constexpr uint32_t kAbs = 0x7fff7fffu;
+    const uint32_t m = __vmaxu2(__vimax3_u16x2(e.a.x & kAbs, e.a.y & kAbs, e.a.z & kAbs), e.a.w & kAbs);
+    return max(m << 16, m & 0xffff0000u);
+}
 // Eight codes of a row, in the same two arrangements.
 template <bool VEC>
 __device__ __forceinline__ uint2 load_codes8(const uint8_t *row, int col, int step, int cols)
@@ -261,41 +274,30 @@ __device__ __forceinline__ void store_codes8(uint8_t *row, int col, int step, in
 }
 
 // Scale byte and codes of eight neighbouring values, given the largest magnitude of their block.  in: the row exists.
-template <bool ALIGNED>
 __device__ __forceinline__ void keep_side8(const Act8View &k, bool in, long long row, int col, int cols, const F2 *v, uint32_t amax)
 {
     const uint32_t byte = act8_scale_byte(amax, k.form);
     const uint2 w = act8_encode8(v, byte, k.form);
     if (!in || col >= cols) return;
     if ((col & 31) == 0) k.scale[row * k.ld_scale + (col >> 5)] = (uint8_t)byte;
-    store_codes8<ALIGNED>(k.code + row * k.ld_code, col, 1, cols, w);
+    store_codes8<true>(k.code + row * k.ld_code, col, 1, cols, w);
 }
 
-// Scale byte and codes of a thread's eight values of a row.  SIDE: they are neighbours, and four threads in a row make a block; else
-// they lie T columns apart, and a block is one value of each lane.  ALIGNED: eight codes may be stored at once (SIDE only).
-// Whole warps; in: the row exists.
-template <bool SIDE, bool ALIGNED, int T>
+// Scale byte and codes of a thread's eight values of a row that lie T columns apart: a block is one value of each lane.  Whole warps.
+template <int T>
 __device__ __forceinline__ void keep8(const Act8View &k, bool in, long long row, int col, int cols, const F2 *v)
 {
-    if (SIDE) {
-        // (values behind the last column are zeros)
-        uint32_t amax = abs_bits_max8(v);
-        amax = max(amax, __shfl_xor_sync(0xffffffffu, amax, 1));
-        amax = max(amax, __shfl_xor_sync(0xffffffffu, amax, 2));
-        keep_side8<ALIGNED>(k, in, row, col, cols, v, amax);
-    } else {
-        uint32_t w[2] = {0u, 0u};
+    uint32_t w[2] = {0u, 0u};
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            const int c = col + j * T;
-            const float x = j & 1 ? hi(v[j >> 1]) : lo(v[j >> 1]);
-            const uint32_t byte = act8_scale_byte(__reduce_max_sync(0xffffffffu, abs_bits(x)), k.form);
-            if (in && (c & 31) == 0 && c < cols) k.scale[row * k.ld_scale + (c >> 5)] = (uint8_t)byte;
-            const F2 one[4] = {f2(x, 0.0f), f2(0.0f), f2(0.0f), f2(0.0f)};
-            w[j >> 2] |= (act8_encode8(one, byte, k.form).x & 255u) << (8 * (j & 3));
-        }
-        if (in) store_codes8<false>(k.code + row * k.ld_code, col, T, cols, make_uint2(w[0], w[1]));
+    for (int j = 0; j < 8; ++j) {
+        const int c = col + j * T;
+        const float x = j & 1 ? hi(v[j >> 1]) : lo(v[j >> 1]);
+        const uint32_t byte = act8_scale_byte(__reduce_max_sync(0xffffffffu, abs_bits(x)), k.form);
+        if (in && (c & 31) == 0 && c < cols) k.scale[row * k.ld_scale + (c >> 5)] = (uint8_t)byte;
+        const F2 one[4] = {f2(x, 0.0f), f2(0.0f), f2(0.0f), f2(0.0f)};
+        w[j >> 2] |= (act8_encode8(one, byte, k.form).x & 255u) << (8 * (j & 3));
     }
+    if (in) store_codes8<false>(k.code + row * k.ld_code, col, T, cols, make_uint2(w[0], w[1]));
 }
 
 // For kernels launched programmatically: they may start while the kernel before them in the stream ends, and wait here for what that

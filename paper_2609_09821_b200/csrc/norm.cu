@@ -108,10 +108,10 @@ __global__ void __launch_bounds__(kThreads) norm_forward_kernel(const NormForwar
 #pragma unroll
                 for (int c = 0; c < C; ++c) amax[c] = max(amax[c], __shfl_xor_sync(0xffffffffu, amax[c], 2));
 #pragma unroll
-                for (int c = 0; c < C; ++c) keep_side8<true>(P.keep, r < P.M, r, first(c), N, v + 4 * c, amax[c]);
+                for (int c = 0; c < C; ++c) keep_side8(P.keep, r < P.M, r, first(c), N, v + 4 * c, amax[c]);
             } else {
 #pragma unroll
-                for (int c = 0; c < C; ++c) keep8<false, false, T>(P.keep, r < P.M, r, first(c), N, v + 4 * c);
+                for (int c = 0; c < C; ++c) keep8<T>(P.keep, r < P.M, r, first(c), N, v + 4 * c);
             }
         }
 #pragma unroll
