@@ -212,6 +212,12 @@ __device__ __forceinline__ void full_store8(float *p, const F2 *v)
 {
     float4 a = make_float4(floored<RELU>(lo(v[0])), floored<RELU>(hi(v[0])), floored<RELU>(lo(v[1])), floored<RELU>(hi(v[1])));
     float4 b = make_float4(floored<RELU>(lo(v[2])), floored<RELU>(hi(v[2])), floored<RELU>(lo(v[3])), floored<RELU>(hi(v[3])));
+    if ((reinterpret_cast<uintptr_t>(p) & 31) == 0) {
+        // a whole sector by one instruction (131072 x 1024 restored as fp32: 111 us, by two stores of half a sector each 143)
+        asm volatile("st.global.v8.f32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "f"(a.x), "f"(a.y), "f"(a.z), "f"(a.w), "f"(b.x), "f"(b.y),
+                     "f"(b.z), "f"(b.w) : "memory");
+        return;
+    }
     reinterpret_cast<float4 *>(p)[0] = a;
     reinterpret_cast<float4 *>(p)[1] = b;
 }

@@ -329,3 +329,31 @@ def test_tensors_that_do_not_fit_are_refused():
         B.layer_norm(torch.zeros(2, 8200, device="cuda"), None, None, torch.zeros(2, 8200, device="cuda"))
     with pytest.raises(B.ImError):
         B.layer_norm(torch.zeros(0, 8, device="cuda"), None, None, torch.zeros(0, 8, device="cuda"))
+
+
+@pytest.mark.parametrize("N", [64, 360, 1024, 2052])
+@pytest.mark.parametrize("pad,shift", [(0, 4), (4, 0), (4, 4), (12, 8)])
+def test_fp32_rows_at_half_a_sector_hold_the_same_bits(N, pad, shift):
+    """fp32 rows that start at a multiple of 16 bytes but not of 32 (all of them, or every other one) are written by other
+    instructions: the values are the same, and so is all around them."""
+    M = 77
+    g = torch.Generator(device="cuda").manual_seed(N + pad)
+    x, dy = (torch.randn(M, N, device="cuda", generator=g) for _ in range(2))
+    gamma, beta = (torch.randn(N, device="cuda", generator=g) for _ in range(2))
+    got = []
+    for p, s in ((24, 0), (pad, shift)):
+        p += -(N + p) % 4                                      # (rows of a multiple of 16 bytes in both)
+        y, sy = matrix(M, N, torch.float32, p, s)
+        dx, sdx = matrix(M, N, torch.float32, p, s)
+        back, sback = matrix(M, N, torch.float32, p, s)
+        mean, rstd = torch.empty(2, M, device="cuda")
+        ck = B.Act8.empty(M, N, "int8")
+        dgamma, dbeta = torch.empty(2, N, device="cuda")
+        B.layer_norm(x, gamma, beta, y, mean, rstd, relu=True, ckpt=ck)
+        B.layer_norm_backward(dy, gamma, beta, rstd, dx, dgamma, dbeta, B.layer_norm_workspace(M, N), relu=True, x=x, mean=mean)
+        B.act8_unpack(ck, back, gamma, beta, relu=True)
+        for view, storage in ((y, sy), (dx, sdx), (back, sback)):
+            assert untouched(view, storage)
+        got.append([t.clone() for t in (y, dx, back, dgamma, dbeta)])
+    for a, b in zip(*got):
+        assert torch.equal(a, b)
