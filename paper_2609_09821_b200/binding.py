@@ -712,7 +712,8 @@ def _here() -> int:
 
 
 def _on(stream, dev: int) -> int:
-    return (_torch.cuda.current_stream(dev) if stream is None else stream).cuda_stream
+    # (the raw handle at once: current_stream() builds a Stream object around it, 1.2 us of a call's 9.6)
+    return _torch._C._cuda_getCurrentRawStream(dev) if stream is None else stream.cuda_stream
 
 
 def _mat(t, what: str, dev: int, rows=None, cols=None, types=_FLOATS):
