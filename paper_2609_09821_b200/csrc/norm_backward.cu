@@ -153,7 +153,7 @@ __global__ void __launch_bounds__(cta_threads(T), 512 / cta_threads(T)) norm_bac
             for (int i = 0; i < R; ++i)
                 if (base + (long long)i * kGroups + g >= P.M) {
 #pragma unroll
-                    for (int e = 0; e < E; ++e) h[i][e] = f2(0.0f);
+                    for (int e = 0; e < E; ++e) h[i][e] = xh[i][e] = f2(0.0f);
                 }
         }
 #pragma unroll
@@ -161,6 +161,7 @@ __global__ void __launch_bounds__(cta_threads(T), 512 / cta_threads(T)) norm_bac
             F2 s1 = f2(0.0f), s2 = f2(0.0f);
 #pragma unroll
             for (int e = 0; e < E; ++e) {
+                if (VEC && C > 1 && e % 4 == 0 && first(e / 4) >= N) break;
                 if (RELU) {
                     const F2 y = fma2(ga[e], xh[i][e], be[e]);
                     h[i][e] = f2(lo(y) > 0.0f ? lo(h[i][e]) : 0.0f, hi(y) > 0.0f ? hi(h[i][e]) : 0.0f);
@@ -171,8 +172,10 @@ __global__ void __launch_bounds__(cta_threads(T), 512 / cta_threads(T)) norm_bac
                 acc_b[e] = add2(acc_b[e], h[i][e]);
                 acc_g[e] = fma2(h[i][e], xh[i][e], acc_g[e]);
             }
-            s[2 * i] = lo(s1) + hi(s1);
-            s[2 * i + 1] = lo(s2) + hi(s2);
+            // (VEC: a thread behind the last column holds the first ones again, which may be infinite)
+            const bool counts = !VEC || C > 1 || first(0) < N;
+            s[2 * i] = counts ? lo(s1) + hi(s1) : 0.0f;
+            s[2 * i + 1] = counts ? lo(s2) + hi(s2) : 0.0f;
         }
         const float one = lane_sums<T>(s);
         if (T == 32) {

@@ -357,3 +357,36 @@ def test_fp32_rows_at_half_a_sector_hold_the_same_bits(N, pad, shift):
         got.append([t.clone() for t in (y, dx, back, dgamma, dbeta)])
     for a, b in zip(*got):
         assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("kept", [False, True])
+@pytest.mark.parametrize("N", [72, 40, 264, 520, 1032, 2056, 4104, 6000])
+def test_an_infinite_gradient_spoils_its_row_as_the_formula_says(N, kept):
+    """One infinity among the first columns of dy: dx of its row holds the infinities and NaNs that the formula gives (threads
+    behind the last column add nothing to the row's sums), dgamma and dbeta of its column are infinite, all else is finite."""
+    M, row, col = 13, 3, 2
+    g = torch.Generator(device="cuda").manual_seed(N)
+    x, dy = (torch.randn(M, N, device="cuda", generator=g) for _ in range(2))
+    gamma = torch.rand(N, device="cuda", generator=g) + 0.5
+    x[row, col] = 3.0
+    dy[row, col] = float("inf")
+    y, dx = torch.empty_like(x), torch.empty_like(x)
+    mean, rstd = torch.empty(2, M, device="cuda")
+    dgamma, dbeta = torch.empty(2, N, device="cuda")
+    ck = B.Act8.empty(M, N, "int8")
+    B.layer_norm(x, gamma, None, y, mean, rstd, ckpt=ck)
+    B.layer_norm_backward(dy, gamma, None, rstd, dx, dgamma, dbeta, B.layer_norm_workspace(M, N), **(dict(ckpt=ck) if kept else dict(x=x, mean=mean)))
+    xh = (x - mean[:, None]) * rstd[:, None]
+    if kept:
+        xh = torch.empty_like(x)
+        B.act8_unpack(ck, xh)
+    gh = dy.double() * gamma.double()
+    c1, c2 = gh.mean(1, keepdim=True), (gh * xh.double()).mean(1, keepdim=True)
+    want = rstd.double()[:, None] * (gh - c1 - xh.double() * c2)
+    assert torch.equal(want.isnan(), dx.isnan())
+    assert torch.equal(want.isneginf(), dx.isneginf()) and torch.equal(want.isposinf(), dx.isposinf())
+    others = torch.arange(M, device="cuda") != row
+    assert bool(dx[others].isfinite().all())
+    for t in (dgamma, dbeta):
+        assert float(t[col]) == float("inf")
+        assert int((~t.isfinite()).sum()) == 1
