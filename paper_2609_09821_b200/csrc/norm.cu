@@ -255,11 +255,12 @@ im_status im_layer_norm_backward(int32_t M, int32_t N, const void *dy, int64_t l
     a.dy = dy; a.x = x; a.dx = dx; a.ld_dy = ld_dy; a.ldx = ldx; a.ld_dx = ld_dx; a.M = M; a.N = N; a.relu = relu != 0;
     a.mean = mean; a.rstd = rstd; a.gamma = gamma; a.beta = beta; a.kept = act8_view(kept);
     a.partial = sums ? static_cast<float *>(workspace) : nullptr;
+    a.dgamma = dgamma; a.dbeta = dbeta; a.finish = 0;
     int n_partials = 0;
     cudaStream_t st = (cudaStream_t)cuda_stream;
     cudaError_t e = launch_norm_backward(a, x_dtype, dy_dtype, n_sm, &n_partials, st);
     g_launches.fetch_add(1, std::memory_order_relaxed);
-    if (e == cudaSuccess && sums) {
+    if (e == cudaSuccess && n_partials > 0) {
         e = launch_pdl(norm_finish_kernel, dim3((unsigned)((2 * N + 31) / 32)), dim3(32, kFinishParts), 0, st, 0, (const float *)a.partial, n_partials, N, dgamma, dbeta);
         g_launches.fetch_add(1, std::memory_order_relaxed);
     }

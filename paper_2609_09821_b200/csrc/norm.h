@@ -28,10 +28,12 @@ struct NormBackward {
     const float *mean, *rstd, *gamma, *beta;
     Act8View kept;
     float *partial;                        // [gridDim.x][2][N] column sums of h xh and of h, or null
+    float *dgamma, *dbeta;                 // [N] or null
+    int finish;                            // > 0 (the launcher's): the grid is one cluster; the first `finish` CTAs have rows, all add up the sums
 };
 
 cudaError_t launch_norm_forward(const NormForward &a, int x_dtype, int y_dtype, int n_sm, cudaStream_t stream);
-// *n_partials: the rows of a.partial written
+// *n_partials: the rows of a.partial that are still to be added up (0: dgamma and dbeta are done)
 cudaError_t launch_norm_backward(const NormBackward &a, int x_dtype, int dy_dtype, int n_sm, int *n_partials, cudaStream_t stream);
 
 }  // namespace im

@@ -7,7 +7,7 @@
 // normalised to, so the ReLU opens the same elements; or from an 8-bit checkpoint of it.
 // A thread owns eight columns for the whole launch: their share of dgamma and dbeta stays in registers over all rows that
 // the CTA walks, and is written once, as one row of partial sums per CTA (summed in fp64 in a fixed order by a second
-// kernel, so results are bit-reproducible).  The two row means are sums over the 8 to 512 threads of a row.
+// kernel, or by the CTAs themselves where few hold all rows, so results are bit-reproducible).  The two row means are sums over the 8 to 512 threads of a row.
 // x (or its codes) and dy are read once, dx is written once.  131072 x 1024 from int8, dy and dx bf16: 142 us, 4.7 TB/s; what bounds it is
 // issue slots (62 %) between the barriers of two rows.  One row per barrier 193 us, four (spilled) 288, a warp per row with 32
 // columns a lane 236.
@@ -17,6 +17,11 @@
 namespace im {
 
 namespace {
+
+// Where eight CTAs hold all rows at once, they are one cluster and finish the column sums themselves: a second kernel costs more than the
+// barrier (64 x 512 fp32: 4.4 us to 4.3, and a call 12.5 us to 10.3; 32 x 1024: 5.0 to 5.2, 12.6 to 10.3).  Not for wider rows (16 x 2048:
+// 6.0 to 7.0), nor for two batches of rows a CTA (128 x 512: 4.5 to 5.1).
+constexpr int kCluster = 8;
 
 constexpr __host__ __device__ int cta_threads(int T) { return T > 256 ? T : 256; }
 
@@ -249,7 +254,7 @@ __global__ void __launch_bounds__(cta_threads(T), 512 / cta_threads(T)) norm_bac
             }
         }
     }
-    if (g == 0) {
+    if (g == 0 && (!P.finish || (int)blockIdx.x < P.finish)) {
 #pragma unroll
         for (int e = 0; e < E; ++e)
 #pragma unroll
@@ -261,6 +266,19 @@ __global__ void __launch_bounds__(cta_threads(T), 512 / cta_threads(T)) norm_bac
                 }
             }
     }
+    if (!P.finish) return;
+    // (CTAs without rows have come here too: they take their share of the columns)
+    asm volatile("barrier.cluster.arrive.release;\n\tbarrier.cluster.wait.acquire;" ::: "memory");
+    for (int k = (int)blockIdx.x * kCta + threadIdx.x; k < 2 * N; k += (int)gridDim.x * kCta) {
+        float v[kCluster];
+#pragma unroll
+        for (int i = 0; i < kCluster; ++i) v[i] = i < P.finish ? __ldcg(P.partial + (long long)i * 2 * N + k) : 0.0f;
+        double s = 0.0;
+#pragma unroll
+        for (int i = 0; i < kCluster; ++i) s += (double)v[i];
+        float *out = k < N ? P.dgamma : P.dbeta;
+        if (out) out[k < N ? k : k - N] = (float)s;
+    }
 }
 
 template <typename TX, typename TY, bool VEC, int T, int C, int R, bool KEPT, bool RELU>
@@ -268,10 +286,16 @@ cudaError_t launch_backward(const NormBackward &a, int n_sm, int *n_partials, cu
 {
     constexpr int kGroups = cta_threads(T) / T;
     const long long want = ((long long)a.M + kGroups * R - 1) / (kGroups * R);
+    if (a.partial && want <= kCluster && T <= 128) {
+        NormBackward b = a;
+        b.finish = (int)want;
+        *n_partials = 0;
+        return launch_pdl(norm_backward_kernel<TX, TY, VEC, T, C, R, KEPT, RELU>, dim3(kCluster), dim3(cta_threads(T)), 0, stream, kCluster, b);
+    }
     long long most = (long long)n_sm * (512 / cta_threads(T));
     most = most < kNormMaxPartials ? most : kNormMaxPartials;
     const int grid = (int)(want < most ? want : most);
-    *n_partials = grid;
+    *n_partials = a.partial ? grid : 0;
     return launch_pdl(norm_backward_kernel<TX, TY, VEC, T, C, R, KEPT, RELU>, dim3((unsigned)grid), dim3(cta_threads(T)), 0, stream, 0, a);
 }
 template <typename TX, typename TY, bool KEPT, bool RELU>

@@ -390,3 +390,31 @@ def test_an_infinite_gradient_spoils_its_row_as_the_formula_says(N, kept):
     for t in (dgamma, dbeta):
         assert float(t[col]) == float("inf")
         assert int((~t.isfinite()).sum()) == 1
+
+
+@pytest.mark.parametrize("N", [8, 64, 200, 361, 512, 1000, 1024, 1032])
+@pytest.mark.parametrize("M", [1, 2, 5, 8, 9, 32, 33, 64, 65])
+def test_few_rows_column_sums(M, N):
+    """Batches on both sides of the size up to which one launch does all: column sums against 64 bits, twice the same bits, no
+    workspace beyond what was asked for, either of the two left out."""
+    g = torch.Generator(device="cuda").manual_seed(M * N)
+    x, dy = (torch.randn(M, N, device="cuda", generator=g) for _ in range(2))
+    y, dx = torch.empty_like(x), torch.empty_like(x)
+    mean, rstd = torch.empty(2, M, device="cuda")
+    B.layer_norm(x, None, None, y, mean, rstd)
+    need = B.layer_norm_workspace(M, N).numel()
+    store = torch.full((need + 256,), 170, dtype=torch.uint8, device="cuda")
+    out = []
+    for which in (3, 3, 1, 2):
+        sums = torch.full((2, N), SENTINEL, device="cuda")
+        B.layer_norm_backward(dy, None, None, rstd, dx, sums[0] if which & 1 else None, sums[1] if which & 2 else None, store[:need], x=x, mean=mean)
+        out.append(sums)
+    assert bool((store[need:] == 170).all())
+    assert torch.equal(out[0], out[1])
+    assert torch.equal(out[2][0], out[0][0]) and bool((out[2][1] == SENTINEL).all())
+    assert torch.equal(out[3][1], out[0][1]) and bool((out[3][0] == SENTINEL).all())
+    # products exact to U each (the same xh, in fp32), sums of at most M terms in fp32
+    xh = ((x - mean[:, None]) * rstd[:, None]).double()
+    terms = dy.double() * xh
+    assert bool(((out[0][0].double() - terms.sum(0)).abs() <= (M + 2) * ref.U * terms.abs().sum(0) + 1e-30).all())
+    assert bool(((out[0][1].double() - dy.double().sum(0)).abs() <= (M + 2) * ref.U * dy.double().abs().sum(0) + 1e-30).all())
