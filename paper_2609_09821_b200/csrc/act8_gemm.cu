@@ -168,12 +168,18 @@ __device__ __forceinline__ void tmem_ld16_issue(uint32_t taddr, float (&v)[16])
 }
 // Bounded wait of a whole warp (the same answer in every lane): false when the limit ran out or another role gave up.  The hint lets
 // the hardware hold the warp for up to 20 us at a time: warps that spin take issue slots from those that restore.
+// FROM_PEER: threads of the other CTA of the pair arrive on the barrier too, so what it hands over is acquired at cluster scope.
+template <bool FROM_PEER = false>
 __device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity, volatile int *abort_flag)
 {
     const auto try_once = [&]() {
         uint32_t ok;
-        asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\n\tvote.sync.all.pred p, p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}"
-                     : "=r"(ok) : "r"(bar), "r"(parity), "r"(20000u) : "memory");
+        if (FROM_PEER)
+            asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2, %3;\n\tvote.sync.all.pred p, p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}"
+                         : "=r"(ok) : "r"(bar), "r"(parity), "r"(20000u) : "memory");
+        else
+            asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\n\tvote.sync.all.pred p, p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}"
+                         : "=r"(ok) : "r"(bar), "r"(parity), "r"(20000u) : "memory");
         return ok != 0;
     };
     if (try_once()) return true;
@@ -192,13 +198,16 @@ __device__ __forceinline__ bool elect_one()
     asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(p));
     return p != 0;
 }
-// Arrives on a barrier of the pair's leader (map_to_rank).  What a restoring warp publishes by it lies in its own CTA's shared
-// memory and is read there by that SM's tensor core, for which fence.proxy.async has ordered it before the arrive; a release at
-// cluster scope on top costs each k-block 900 cycles and more (measured; it waits for the thread's loads in flight), twice the
-// rest of the work.
-__device__ __forceinline__ void mbar_arrive_remote(uint32_t cluster_addr)
+// Arrives on a barrier of the pair's leader (map_to_rank), whose MMA warp acquires at cluster scope: a release at cluster scope of
+// shared memory alone.  Restored tiles need no more: they lie in this CTA's shared memory, fence.proxy.async has ordered them before the
+// tensor core's reads, and the other lanes' share is ordered by the __syncwarp before this lane's release.  Nor do emptied accumulators:
+// the loads from tensor memory are complete (tcgen05.wait::ld) and ordered before the arrive by tcgen05.fence, as the MMAs that
+// overwrite them are behind the wait.  An arrive.release.cluster releases global memory too and waits for all of it, about 1 us:
+// 131072 x 1024 x 1024 410 us with it for the tiles (450 by one warp for all of a k-block) and 260 for the accumulators alone, 249 with this.
+__device__ __forceinline__ void mbar_arrive_shared_to_peer(uint32_t cluster_addr)
 {
-    asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(cluster_addr) : "memory");
+    asm volatile("fence.release.sync_restrict::shared::cta.cluster;" ::: "memory");
+    asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(cluster_addr) : "memory");
 }
 __device__ __forceinline__ void mbar_arrive_addr(uint32_t addr) { asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(addr) : "memory"); }
 
@@ -282,9 +291,9 @@ __device__ __forceinline__ void act8_tn_body(const CUtensorMap &map_a, const CUt
                 int in_chain = 0;
                 for (int i = 0; i < part.n; ++i) {
                     if (in_chain == 0) {
-                        if (!(ok = warp_wait(smem_u32(&acc_empty[acc]), acc_phase ^ 1u, abort_flag))) break;
+                        if (!(ok = warp_wait<PAIR>(smem_u32(&acc_empty[acc]), acc_phase ^ 1u, abort_flag))) break;
                     }
-                    if (!(ok = warp_wait(smem_u32(&full[stage]), phase, abort_flag))) break;
+                    if (!(ok = warp_wait<PAIR>(smem_u32(&full[stage]), phase, abort_flag))) break;
                     tc_fence_after();
                     const uint32_t d = tmem_base + (uint32_t)(acc * BLOCK_N);
                     const uint64_t step = (uint64_t)(uint32_t)(stage * (PL::kStageBytes >> 4)), dh = dh0 + step, da = da0 + step;
@@ -360,7 +369,7 @@ __device__ __forceinline__ void act8_tn_body(const CUtensorMap &map_a, const CUt
         const uint32_t tile0 = smem_u32(tiles) + (uint32_t)(half * 8192 + r * 128) + (uint32_t)((cq ^ (r & 7)) << 4);
         const uint32_t raw0 = smem_u32(raw) + (uint32_t)(r * 128) + (uint32_t)(((half * 4 + (cq >> 1)) ^ (r & 7)) << 4) + (uint32_t)((cq & 1) * 8);
         const uint32_t scale0 = smem_u32(scales) + (uint32_t)(r * 4 + half * 2 + (cq >> 2));
-        const uint32_t full0 = PAIR ? map_to_rank(smem_u32(full), 0) : smem_u32(full), raw_full0 = smem_u32(raw_full), raw_empty0 = smem_u32(raw_empty), empty0 = smem_u32(empty);
+        const uint32_t full0 = PAIR && rank == 1 ? map_to_rank(smem_u32(full), 0) : smem_u32(full), raw_full0 = smem_u32(raw_full), raw_empty0 = smem_u32(raw_empty), empty0 = smem_u32(empty);
         int taken = 0, slot = group;
         uint32_t raw_phase = 0;
         stage = group;
@@ -400,7 +409,7 @@ __device__ __forceinline__ void act8_tn_body(const CUtensorMap &map_a, const CUt
                 __syncwarp();
                 if (lane == 0) {
                     mbar_arrive_addr(raw_empty0 + (uint32_t)(slot * 8));
-                    if (PAIR) mbar_arrive_remote(full0 + (uint32_t)(stage * 8));
+                    if (PAIR && rank == 1) mbar_arrive_shared_to_peer(full0 + (uint32_t)(stage * 8));
                     else mbar_arrive_addr(full0 + (uint32_t)(stage * 8));
                 }
                 stage += 2;
@@ -451,7 +460,7 @@ __device__ __forceinline__ void act8_tn_body(const CUtensorMap &map_a, const CUt
                 tc_fence_before();
                 __syncwarp();
                 if (lane == 0) {
-                    if (PAIR) mbar_arrive_remote(map_to_rank(smem_u32(&acc_empty[acc]), 0));
+                    if (PAIR && rank == 1) mbar_arrive_shared_to_peer(map_to_rank(smem_u32(&acc_empty[acc]), 0));
                     else mbar_arrive(&acc_empty[acc]);
                 }
                 if (++acc == PL::kAccs) { acc = 0; acc_phase ^= 1u; }
