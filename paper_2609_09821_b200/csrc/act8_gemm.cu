@@ -433,10 +433,13 @@ __device__ __forceinline__ void act8_tn_body(const CUtensorMap &map_a, const CUt
                 if (!(ok = warp_wait(smem_u32(&acc_full[acc]), acc_phase, abort_flag))) break;
                 tc_fence_after();
                 const uint32_t t_quad = tmem_base + ((uint32_t)(quad * 32) << 16), t_row = t_quad + (uint32_t)(acc * BLOCK_N), t_sum = t_quad + (uint32_t)(PL::kAccs * BLOCK_N);
-                // 32 columns at a time: the accumulator plus the sum so far, back into the sum, or out if it is the last chain
+                // 32 columns at a time: the accumulator plus the sum so far, back into the sum, or out if it is the last chain.  (c0 is hidden
+                // from the compiler: where there is one step, on 64-column tiles, it would form all 32 addresses before the first chain
+                // and spill 216 bytes next to registers that tensor-memory loads are writing.)
                 const bool first = i0 == 0, last = i0 + kChainBlocks >= part.n;
 #pragma unroll 1
                 for (int c0 = c_first; c0 < c_first + BLOCK_N / 2; c0 += 32) {
+                    asm volatile("" : "+r"(c0));
                     float v[32];
                     tmem_ld32_issue(t_row + (uint32_t)c0, v);
                     if (!first) {
