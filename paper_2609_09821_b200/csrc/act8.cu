@@ -118,7 +118,7 @@ int row_threads_bits(int N, bool vec)
 dim3 grid_for(int M, int N, int tx_bits, int rows_at_once, int n_sm)
 {
     const int rows_per_cta = kThreads >> tx_bits;
-    const unsigned gx = (unsigned)((N + (8 << tx_bits) - 1) / (8 << tx_bits));
+    const unsigned gx = (unsigned)(((long long)N + (8 << tx_bits) - 1) / (8 << tx_bits));     // (so many that no thread's columns pass 2^31 - 1)
     long long gy = ((long long)M + rows_per_cta * rows_at_once - 1) / (rows_per_cta * rows_at_once);
     const long long most = ((long long)n_sm * 16 + gx - 1) / gx;         // beyond that each thread walks more rows
     gy = gy < most ? gy : most;

@@ -23,7 +23,7 @@ struct Act8View {                          // im_act8 as the kernels take it
 inline bool act8_valid(const im_act8 *a, int cols)
 {
     return a && a->code && a->scale && (a->form == IM_ACT8_INT8 || a->form == IM_ACT8_E4M3) && a->ld_code >= cols &&
-           a->ld_scale >= (cols + kActBlock - 1) / kActBlock;
+           a->ld_scale >= ((int64_t)cols + kActBlock - 1) / kActBlock;
 }
 inline Act8View act8_view(const im_act8 *a)
 {
@@ -184,7 +184,7 @@ __device__ __forceinline__ Eight<__nv_bfloat16> full8(const __nv_bfloat16 *p) { 
 template <bool VEC, typename T>
 __device__ __forceinline__ Eight<T> load8(const T *row, int col, int step, int cols)
 {
-    if (VEC && col + 8 <= cols) return full8(row + col);
+    if (VEC && col <= cols - 8) return full8(row + col);
     Eight<T> e = zero8(row);
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
@@ -229,7 +229,7 @@ __device__ __forceinline__ void full_store8(__nv_bfloat16 *p, const F2 *v)
 template <bool VEC, bool RELU, typename T>
 __device__ __forceinline__ void store8(T *row, int col, int step, int cols, const F2 *v)
 {
-    if (VEC && col + 8 <= cols) {
+    if (VEC && col <= cols - 8) {
         full_store8<RELU>(row + col, v);
         return;
     }
@@ -256,7 +256,7 @@ __device__ __forceinline__ uint32_t largest8(const Eight<__nv_bfloat16> &e)
 template <bool VEC>
 __device__ __forceinline__ uint2 load_codes8(const uint8_t *row, int col, int step, int cols)
 {
-    if (VEC && col + 8 <= cols) return __ldcs(reinterpret_cast<const uint2 *>(row + col));
+    if (VEC && col <= cols - 8) return __ldcs(reinterpret_cast<const uint2 *>(row + col));
     uint32_t w[2] = {0u, 0u};
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
@@ -268,7 +268,7 @@ __device__ __forceinline__ uint2 load_codes8(const uint8_t *row, int col, int st
 template <bool VEC>
 __device__ __forceinline__ void store_codes8(uint8_t *row, int col, int step, int cols, uint2 w)
 {
-    if (VEC && col + 8 <= cols) {
+    if (VEC && col <= cols - 8) {
         *reinterpret_cast<uint2 *>(row + col) = w;
         return;
     }
