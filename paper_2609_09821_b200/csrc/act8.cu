@@ -160,7 +160,7 @@ im_status im_act8_unpack(int32_t M, int32_t N, const im_act8 *in, const float *g
                          int32_t out_dtype, void *cuda_stream)
 {
     using namespace im;
-    if (!out || M < 1 || N < 1 || ld_out < N || !float_dtype(out_dtype) || !aligned_to(out, dtype_size(out_dtype)) || !act8_valid(in, N)) return IM_ERR_INVALID_ARG;
+    if (!out || M < 1 || N < 1 || ld_out < N || !float_dtype(out_dtype) || !aligned_to(out, dtype_size(out_dtype)) || !words(gamma, beta) || !act8_valid(in, N)) return IM_ERR_INVALID_ARG;
     const int n_sm = device_sm_count();
     if (n_sm <= 0) return IM_ERR_UNSUPPORTED;
     const Act8View v = act8_view(in);

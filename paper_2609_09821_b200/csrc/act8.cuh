@@ -315,6 +315,9 @@ __device__ __forceinline__ void after_previous_kernel()
 }
 
 inline bool aligned_to(const void *p, uintptr_t bytes) { return (reinterpret_cast<uintptr_t>(p) & (bytes - 1)) == 0; }
+// Whether all of these (any of them null) may hold 32-bit values.
+template <typename... P>
+inline bool words(const P *...p) { return (aligned_to(p, 4) && ...); }
 inline size_t dtype_size(int dtype) { return dtype == IM_DTYPE_F32 ? 4 : 2; }
 inline bool float_dtype(int dtype) { return dtype == IM_DTYPE_F32 || dtype == IM_DTYPE_BF16; }
 // Whether every row of [.][ld] starts on 16 bytes.

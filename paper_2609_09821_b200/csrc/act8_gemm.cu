@@ -635,7 +635,7 @@ im_status im_gemm_act8_tn(const uint16_t *A, int64_t lda, const im_act8 *H, floa
                           const float *beta, int32_t relu, void *workspace, size_t workspace_bytes, uint32_t *status, void *cuda_stream)
 {
     using namespace im;
-    if (!A || !C || !status || R < 1 || Mo < 1 || No < 1 || lda < Mo || ldc < No || (lda & 7) || !aligned_to(A, 16) || !aligned_to(C, 4)) return IM_ERR_INVALID_ARG;
+    if (!A || !C || !status || R < 1 || Mo < 1 || No < 1 || lda < Mo || ldc < No || (lda & 7) || !aligned_to(A, 16) || !words(C, gamma, beta, status)) return IM_ERR_INVALID_ARG;
     if (!act8_valid(H, No) || (H->ld_code & 15) || !aligned_to(H->code, 16)) return IM_ERR_INVALID_ARG;
     if (Mo > kMaxCols || No > kMaxCols || R > kMaxRows) return IM_ERR_UNSUPPORTED;
     const size_t need = im_gemm_act8_tn_workspace_bytes(R, Mo, No);

@@ -218,7 +218,7 @@ im_status im_layer_norm_forward(int32_t M, int32_t N, const void *x, int64_t ldx
 {
     using namespace im;
     if (!x || !y || M < 1 || N < 1 || ldx < N || ldy < N || !float_dtype(x_dtype) || !float_dtype(y_dtype) || !(eps > 0.0f) || std::isinf(eps)) return IM_ERR_INVALID_ARG;
-    if (!aligned_to(x, dtype_size(x_dtype)) || !aligned_to(y, dtype_size(y_dtype))) return IM_ERR_INVALID_ARG;
+    if (!aligned_to(x, dtype_size(x_dtype)) || !aligned_to(y, dtype_size(y_dtype)) || !words(gamma, beta, mean, rstd)) return IM_ERR_INVALID_ARG;
     if (keep && !act8_valid(keep, N)) return IM_ERR_INVALID_ARG;
     if (N > kNormMaxCols) return IM_ERR_UNSUPPORTED;
     const int n_sm = device_sm_count();
@@ -247,6 +247,7 @@ im_status im_layer_norm_backward(int32_t M, int32_t N, const void *dy, int64_t l
     if (!dy || !rstd || M < 1 || N < 1 || ld_dy < N || !float_dtype(x_dtype) || !float_dtype(dy_dtype) || (!dx && !sums)) return IM_ERR_INVALID_ARG;
     if (!x == !kept || (x && (!mean || ldx < N)) || (kept && !act8_valid(kept, N)) || (dx && ld_dx < N)) return IM_ERR_INVALID_ARG;
     if (!aligned_to(dy, dtype_size(dy_dtype)) || !aligned_to(x, dtype_size(x_dtype)) || !aligned_to(dx, dtype_size(x_dtype))) return IM_ERR_INVALID_ARG;
+    if (!words(mean, rstd, gamma, beta, dgamma, dbeta)) return IM_ERR_INVALID_ARG;
     if (sums && (!workspace || !aligned_to(workspace, 16) || workspace_bytes < im_layer_norm_workspace_bytes(M, N))) return IM_ERR_INVALID_ARG;
     if (N > kNormMaxCols) return IM_ERR_UNSUPPORTED;
     const int n_sm = device_sm_count();
