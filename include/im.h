@@ -562,6 +562,7 @@ im_status im_colsum_f32(const float *x, int64_t ld, int64_t rows, int32_t cols, 
  * elements; matrices are row-major; rows that start on 16 bytes are read and written in 16-byte pieces, others element by element
  * (slower, the same results but for the order of sums).  Columns beyond N are neither read nor written.  All arithmetic and
  * all sums are fp32 (batch sums are finished in fp64); results are bit-reproducible.  NaN and infinities are carried through.
+ * Pointers are aligned to their elements (float vectors and status words to 4 bytes), and more where it is said.
  *
  * im_act8: a matrix in 8 bits.  Columns 32 b .. 32 b + 31 of a row (fewer at its end) share a power of two 2^e, the least
  * with e >= -100 for which the largest magnitude among them is at most 127 2^e (IM_ACT8_INT8) or 448 2^e (IM_ACT8_E4M3); a code is
@@ -588,7 +589,7 @@ im_status im_colsum_f32(const float *x, int64_t ld, int64_t rows, int32_t cols, 
  * im_gemm_act8_tn: the weight gradient of the layer above,  C[n][k] = sum_r A[r][n] H[r][k],  n < Mo, k < No, on the
  *   tensor cores with H restored on the way in: the values im_act8_unpack would give as bf16.  A bf16 [R][lda] (lda a multiple of 8,
  *   16-byte aligned), C float [Mo][ldc].  H->code 16-byte aligned with ld_code a multiple of 16 and whole rows readable (R ld_code
- *   bytes).  R, Mo and No need not be multiples of anything; Mo, No <= 65536, R < 2^31 - 2^16, H's strides < 2^31 (IM_ERR_UNSUPPORTED beyond).  workspace: as
+ *   bytes).  R, Mo and No need not be multiples of anything; Mo, No <= 65536, R <= 2^31 - 2^16, lda < 2^39, H->ld_code < 2^40 (IM_ERR_UNSUPPORTED beyond).  workspace: as
  *   above, im_gemm_act8_tn_workspace_bytes(R, Mo, No) bytes (which may be 0: then NULL will do).  status DEVICE uint32 [1] receives
  *   IM_DEV_WAIT_TIMEOUT if a bounded wait inside the kernel runs out. */
 #define IM_DTYPE_F32  0

@@ -52,6 +52,7 @@ static_assert(kRaw % 2 == 0, "a slot belongs to one group");
 constexpr int kRawBytes = kBlockRows * kTileK, kScaleBytes = kBlockRows * (kTileK / kActBlock);
 constexpr int kMaxCols = 65536;            // of either operand
 constexpr int kMaxRows = 0x7fff0000;       // row numbers (a k-block beyond the last) in 32 bits
+constexpr int64_t kMaxStrideBytes = 1ll << 40;       // a tensor map's row strides are below
 constexpr size_t kSmemLimit = 232448;
 
 struct Act8GemmParams {
@@ -637,7 +638,7 @@ im_status im_gemm_act8_tn(const uint16_t *A, int64_t lda, const im_act8 *H, floa
     using namespace im;
     if (!A || !C || !status || R < 1 || Mo < 1 || No < 1 || lda < Mo || ldc < No || (lda & 7) || !aligned_to(A, 16) || !words(C, gamma, beta, status)) return IM_ERR_INVALID_ARG;
     if (!act8_valid(H, No) || (H->ld_code & 15) || !aligned_to(H->code, 16)) return IM_ERR_INVALID_ARG;
-    if (Mo > kMaxCols || No > kMaxCols || R > kMaxRows) return IM_ERR_UNSUPPORTED;
+    if (Mo > kMaxCols || No > kMaxCols || R > kMaxRows || lda >= kMaxStrideBytes / 2 || H->ld_code >= kMaxStrideBytes) return IM_ERR_UNSUPPORTED;
     const size_t need = im_gemm_act8_tn_workspace_bytes(R, Mo, No);
     if (need && (!workspace || workspace_bytes < need || !aligned_to(workspace, 16))) return IM_ERR_INVALID_ARG;
     int n_sm = device_sm_count();

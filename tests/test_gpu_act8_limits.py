@@ -33,3 +33,32 @@ def test_widest_rows(cols, shift):
     for c in range(0, cols - 2 ** 24, 2 ** 24 * 7):
         want = ref.kept(noise.repeat(17)[c % noise.numel():][:2 ** 20].view(1, -1), ref.INT8)
         assert torch.equal(x[:, c:c + 2 ** 20].double(), want)
+
+
+def test_product_of_rows_far_apart():
+    # strides beyond 2^31 are addressed in 64 bits; what a tensor map cannot express is refused
+    import ctypes
+    import torch
+    from paper_2609_09821_b200 import binding as B
+    R, Mo, No, far = 3, 40, 200, 2 ** 31 + 32
+    rand = lambda *s: torch.randn(*s, device="cuda")  # noqa: E731
+    A = torch.empty(R, far, device="cuda", dtype=torch.bfloat16)[:, :Mo]
+    code = torch.empty(R, far, device="cuda", dtype=torch.uint8)[:, :No]
+    scale = torch.empty(R, far + 1, device="cuda", dtype=torch.uint8)[:, 1:8]
+    A.copy_(rand(R, Mo))
+    ck = B.Act8(code, scale, No)
+    B.act8_pack(rand(R, No), ck)
+    H = torch.empty(R, No, device="cuda")
+    B.act8_unpack(ck, H)
+    C, status = torch.empty(Mo, No, device="cuda"), torch.zeros(1, dtype=torch.int32, device="cuda")
+    ws = B.gemm_act8_tn_workspace(R, Mo, No)
+    B.gemm_act8_tn(A, ck, C, ws, status)
+    want = A.double().T @ H.double()
+    # products are exact, three of them are added: two roundings or truncations, each a step (2 U) of the sum of magnitudes at most
+    assert bool(((C.double() - want).abs() <= 4 * ref.U * (A.double().abs().T @ H.double().abs())).all()) and int(status) == 0
+    call = lambda lda, ld_code: B.load().im_gemm_act8_tn(A.data_ptr(), lda, ctypes.byref(B.Act8View(code.data_ptr(), ld_code, scale.data_ptr(), far + 1, 0)),  # noqa: E731
+                                                         C.data_ptr(), No, 1, Mo, No, None, None, 0, None, 0, status.data_ptr(), None)
+    assert call(2 ** 39, far) == -6 and call(far, 2 ** 40) == -6
+    assert call(2 ** 39 - 8, far) == 0 and call(far, 2 ** 40 - 16) == 0
+    torch.cuda.synchronize()
+    assert int(status) == 0
