@@ -51,3 +51,34 @@ def check(R, Mo, No, form, gamma=False, beta=False, relu=False, scale=None):
                                           (200000, 100, 1100, ref.INT8), (131072, 65, 64, ref.E4M3), (100000, 300, 700, ref.INT8)])
 def test_sums_of_several_chains(R, Mo, No, form):
     check(R, Mo, No, form)
+
+
+@pytest.mark.parametrize("form", [ref.INT8, ref.E4M3])
+@pytest.mark.parametrize("gamma,beta,relu", [(1, 1, 0), (1, 0, 0), (0, 1, 0), (1, 0, 1), (0, 1, 1), (0, 0, 1)])
+@pytest.mark.parametrize("R,Mo,No", [(1000, 28, 361), (1500, 69, 200), (1201, 300, 700), (7001, 140, 130)])
+def test_every_form_of_the_restored_operand(form, gamma, beta, relu, R, Mo, No):
+    check(R, Mo, No, form, gamma=bool(gamma), beta=bool(beta), relu=bool(relu))
+
+
+@pytest.mark.parametrize("R,Mo,No", [(1000, 28, 361), (1500, 69, 1000), (1201, 300, 700)])
+@pytest.mark.parametrize("off,extra", [(0, 1), (1, 3), (2, 2), (3, 6)])             # of the first scale, and of a row's bytes behind the last
+def test_scales_at_any_address(R, Mo, No, off, extra):
+    def scale(rows, blocks):
+        return torch.full((rows, off + blocks + extra), 77, dtype=torch.uint8, device="cuda")[:, off:]
+    check(R, Mo, No, ref.INT8, gamma=True, beta=True, relu=True, scale=scale)
+    check(R, Mo, No, ref.E4M3, scale=scale)
+
+
+@pytest.mark.parametrize("R,Mo,No", [(300, 40, 200), (300, 100, 200), (300, 200, 200)])
+def test_a_marked_block_under_gamma_and_beta(R, Mo, No):
+    g = torch.Generator("cuda").manual_seed(R)
+    A = torch.randn(R, (Mo + 7) // 8 * 8, device="cuda", generator=g).bfloat16()[:, :Mo]        # (strides of A are multiples of 8)
+    x = torch.randn(R, No, device="cuda", generator=g)
+    x[R - 1, 70] = float("inf")
+    ck = B.Act8.empty(R, No)
+    B.act8_pack(x, ck)
+    ga, be = torch.randn(2, No, device="cuda", generator=g)
+    C, status, ws = torch.empty(Mo, No, device="cuda"), torch.zeros(1, dtype=torch.int32, device="cuda"), B.gemm_act8_tn_workspace(R, Mo, No)
+    for kw in (dict(gamma=ga), dict(beta=be), dict(gamma=ga, beta=be), dict(gamma=ga, beta=be, relu=True)):
+        B.gemm_act8_tn(A, ck, C, ws, status, **kw)
+        assert bool(torch.isnan(C[:, 64:96]).all()) and bool(torch.isfinite(C[:, :64]).all()) and bool(torch.isfinite(C[:, 96:]).all()), kw
