@@ -20,13 +20,14 @@
 // 16000 x 512 x 1024 29 us, of which 12 are products; 65536 x 69 x 512 22 us.  What bounds the large product is the restoring warps,
 // which take two thirds of the issue slots, and the stop at each chain's end.
 //
-// Work is cut along the rows where there are fewer output tiles than SMs.  Each tile's rows are shared out to `slices`
-// workers (a CTA or a pair) in equal ranges, so that workers of different tiles walk the same rows at the same time and share
-// them in L2; workers left over take the last rows of all tiles, in a row.  Partial tiles go to the workspace and a second
-// kernel adds them in a fixed order.
+// Work is cut along the rows where there are fewer output tiles than SMs (act8_split.cuh).  Each tile's rows are shared out to
+// `slices` workers (a CTA or a pair) in equal ranges, so that workers of different tiles walk the same rows at the same time and share
+// them in L2; where that pays, workers left over take the last rows of all tiles, in a row.  Partial tiles go to the workspace and a
+// second kernel adds them in a fixed order.
 #include <cstring>
 
 #include "act8.cuh"
+#include "act8_split.cuh"
 #include "im_internal.h"
 #include "mlp.h"
 #include "tc_ptx.cuh"
@@ -35,8 +36,6 @@ namespace im {
 
 namespace {
 
-constexpr int kTileK = 128;                // columns of H per CTA: the M of the instruction, or half of it
-constexpr int kBlockRows = 64;             // rows of a k-block
 constexpr int kScaleWarps = 2, kDecodeWarps = 16, kGroupWarps = 8, kEpiWarps = 8;   // restoring warps: two groups, k-blocks in turn
 constexpr int kFirstDecode = 2 + kScaleWarps, kFirstEpi = kFirstDecode + kDecodeWarps;
 constexpr int kThreads = 32 * (kFirstEpi + kEpiWarps);
@@ -61,8 +60,7 @@ struct Act8GemmParams {
     int R, Mo, No;                         // rows, columns of A, columns of H
     int tiles_k, tiles, kb;                // tiles along H's columns, all tiles, k-blocks of a tile
     int workers;                           // CTAs or pairs
-    int slices, slice_kb;                  // workers per tile and their k-blocks (slices == 1 and no helpers: kb)
-    int helpers;                           // workers for the k-blocks behind slices * slice_kb of every tile
+    int slices, slice_kb, helpers;         // workers per tile and their k-blocks, and workers left over (act8_split.cuh)
     float *C;
     long long ldc;
     float *partial;                        // [slot][tile rows (n)][tile columns (k)]; null: every part is a whole tile and goes to C
@@ -80,40 +78,6 @@ struct Plan {
     static constexpr size_t kSmemBytes = 1024 + (size_t)kStages * kStageBytes + (size_t)kRaw * (kRawBytes + kScaleBytes) + 512;
     static_assert(kSmemBytes <= kSmemLimit && (2 * kStages + 2 * kRaw + 2 * kAccs + 1) * 8 <= 512, "shared memory plan");
 };
-
-// The k-blocks [k0, k0 + n) of a tile, one after another for a worker; slot: where their sum goes.
-struct Part {
-    int tile, k0, n, slot;
-};
-// i-th part of worker w; false behind its last one.
-__device__ __forceinline__ bool part_at(const Act8GemmParams &P, int w, int i, Part &p)
-{
-    const int mains = P.tiles * P.slices;
-    if (w < mains || !P.helpers) {
-        const int m = w + i * P.workers;
-        if (m >= mains || (P.helpers && i > 0)) return false;
-        const int slice = m / P.tiles;
-        p.tile = m - slice * P.tiles;
-        if (P.helpers) { p.k0 = slice * P.slice_kb; p.n = P.slice_kb; }
-        else {
-            p.k0 = (int)((long long)slice * P.kb / P.slices);
-            p.n = (int)((long long)(slice + 1) * P.kb / P.slices) - p.k0;
-        }
-        p.slot = p.tile * P.slices + slice;
-        return true;
-    }
-    const int h = w - mains, base = P.slices * P.slice_kb, rest = P.kb - base;
-    const long long units = (long long)P.tiles * rest, u1 = (long long)(h + 1) * units / P.helpers;
-    long long u = (long long)h * units / P.helpers;
-    u = i == 0 ? u : (u / rest + i) * rest;                          // (a tile after the first begins at its first block)
-    if (u >= u1) return false;
-    p.tile = (int)(u / rest);
-    const int in = (int)(u - (long long)p.tile * rest);
-    p.k0 = base + in;
-    p.n = (int)min((long long)(rest - in), u1 - u);
-    p.slot = mains + h + p.tile;
-    return true;
-}
 
 // Eight codes of one row to bf16.  MODE 0: code 2^e;  1: gamma code 2^e + beta;  2: the same under a ReLU.
 template <int FORM, int MODE>
@@ -503,7 +467,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) act8_tn
 // C = the partial tiles, added in a fixed order (slices, then helpers).  A warp has 128 columns of a row; with SPLIT the eight warps of a
 // CTA share one row's parts, every eighth each, and their sums are added in order: few tiles have many parts.
 // Launched early (programmatically): it waits for the products, and reads what they wrote by plain loads.
-constexpr int kSplitFrom = 12;             // slices
+// slices from which it pays: 16000 x 300 x 700 (12 slices) 29.9 us and 30.9 without, x 69 x 512 (37) 13.0 and 20.7, x 512 x 1024 (9) 30.5 and 27.7
+constexpr int kSplitFrom = 12;
 template <int BLOCK_N, bool PAIR, bool SPLIT>
 __global__ void __launch_bounds__(256) act8_tn_finish_kernel(const Act8GemmParams P)
 {
@@ -549,41 +514,6 @@ cudaError_t launch_finish(const Act8GemmParams &p, cudaStream_t st)
     const unsigned gx = (unsigned)((p.No + 127) / 128);
     if (p.slices >= kSplitFrom) return launch_pdl(act8_tn_finish_kernel<BLOCK_N, PAIR, true>, dim3(gx, (unsigned)p.Mo), dim3(256), 0, st, 0, p);
     return launch_pdl(act8_tn_finish_kernel<BLOCK_N, PAIR, false>, dim3(gx, (unsigned)((p.Mo + 7) / 8)), dim3(256), 0, st, 0, p);
-}
-
-// Tile shape and split.  Narrow A: one CTA per tile, 64 or 128 columns; else pairs with 256, unless H is too narrow for both CTAs.
-struct Split {
-    int block_n;
-    bool pair;
-    int tiles_k, tiles, kb, workers, slices, slice_kb, helpers;
-    size_t slot_bytes() const { return (size_t)block_n * (pair ? 2 : 1) * kTileK * sizeof(float); }
-    bool whole() const { return slices == 1 && helpers == 0; }
-};
-constexpr int kLeastBlocks = 4;            // k-blocks of a part, at least
-constexpr int kHelpFrom = 32;              // k-blocks per worker from which helpers pay for their extra parts
-Split split_for(int R, int Mo, int No, int ctas)
-{
-    Split s;
-    s.pair = Mo > 128 && No > kTileK;
-    s.block_n = s.pair ? 256 : Mo <= 64 ? 64 : 128;
-    s.workers = s.pair ? ctas / 2 : ctas;
-    const int cols = s.pair ? 2 * kTileK : kTileK;
-    s.tiles_k = (No + cols - 1) / cols;
-    s.tiles = s.tiles_k * ((Mo + s.block_n - 1) / s.block_n);
-    s.kb = (R + kBlockRows - 1) / kBlockRows;
-    const int most = s.kb / kLeastBlocks;
-    s.slices = s.workers / s.tiles;
-    s.slices = s.slices < most ? s.slices : most;
-    s.slices = s.slices < 1 ? 1 : s.slices;
-    s.slice_kb = s.kb;
-    s.helpers = 0;
-    const int left = s.workers - s.tiles * s.slices;
-    const long long share = (long long)s.kb * s.tiles / s.workers;                 // k-blocks per worker, if all are busy
-    if (left > 0 && share >= kHelpFrom && s.workers / s.tiles == s.slices) {
-        s.helpers = left;
-        s.slice_kb = (int)share;
-    }
-    return s;
 }
 
 template <int FORM, int MODE>
