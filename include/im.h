@@ -559,8 +559,9 @@ im_status im_colsum_f32(const float *x, int64_t ld, int64_t rows, int32_t cols, 
  * for updates whose activations should take a quarter of the memory.)  Building blocks beside the products above, for a
  * hidden layer Z = H W^T + b (im_gemm_bf16), Y = relu(gamma xh + beta), xh = (Z - mean) rstd.  Everything is asynchronous on
  * cuda_stream, allocates nothing and is capturable.  x_dtype, y_dtype, ...: IM_DTYPE_F32 or IM_DTYPE_BF16; ld*: row strides in
- * elements; matrices are row-major; rows that start on 16 bytes are read and written in 16-byte pieces, others element by element
- * (slower, the same results but for the order of sums).  Columns beyond N are neither read nor written.  All arithmetic and
+ * elements; matrices are row-major; where every row of every matrix of a call starts on 16 bytes (codes: on 8; and in
+ * im_layer_norm_backward N is a multiple of 8) they are read and written in 16-byte pieces, else element by element (slower, the same
+ * results but for the order of sums).  Columns beyond N are neither read nor written.  All arithmetic and
  * all sums are fp32 (batch sums are finished in fp64); results are bit-reproducible.  NaN and infinities are carried through.
  * Pointers are aligned to their elements (float vectors and status words to 4 bytes), and more where it is said.
  *

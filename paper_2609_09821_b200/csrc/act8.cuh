@@ -1,7 +1,7 @@
 // The 8-bit form of activations (im_act8): 32 consecutive columns of a row share a power of two 2^e, the least with
 // e >= -100 for which the largest magnitude among them fits the code (127 as int8, 448 as e4m3); a code is the value over
 // 2^e, rounded to nearest, ties to even.  A code has at most 7 significant bits, so a restored value is exact in bf16.
-// The scale byte is e + 127 (27 .. 248); 255 marks a block that held an infinity or a NaN and is restored as NaN.
+// The scale byte is e + 127 (27 .. 249, the last for int8 blocks with the largest fp32 numbers); 255 marks a block that held an infinity or a NaN and is restored as NaN.
 #pragma once
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>

@@ -11,13 +11,14 @@
 // fetching half of A's columns: per k-block an SM takes in 16 KB of A and 8 KB of codes in place of 32 + 8 on a 128 x 256 tile of
 // its own, which is all that L2 delivers.
 //
-// A restored value has at most 8 significant bits (act8.cuh), so bf16 operands lose nothing of the codes.  The tensor cores
+// A code has at most 7 significant bits (act8.cuh) and the values under gamma, beta and ReLU are bf16 by definition, so bf16 operands lose
+// nothing.  The tensor cores
 // cut off what their accumulator does not hold rather than rounding it, an error that grows with the number of additions:
 // after kChainBlocks k-blocks the epilogue adds the accumulator to the part's sum, which lies in tensor memory too, and the next chain
 // starts from zero.
 //
-// 131072 x 1024 x 1024 from int8 under gamma, beta and ReLU: 236 us, 1160 TFLOP/s (in a long run, at the power limit, 293);
-// 16000 x 512 x 1024 29 us, of which 12 are products; 65536 x 69 x 512 22 us.  What bounds the large product is the restoring warps,
+// 131072 x 1024 x 1024 from int8 under gamma, beta and ReLU: 237 us, 1160 TFLOP/s (in a long run, at the power limit, 285);
+// 16000 x 512 x 1024 28 us, of which 12 are products; 65536 x 69 x 512 21 us, x 28 x 512 20.  What bounds the large product is the restoring warps,
 // which take two thirds of the issue slots, and the stop at each chain's end.
 //
 // Work is cut along the rows where there are fewer output tiles than SMs (act8_split.cuh).  Each tile's rows are shared out to
@@ -41,7 +42,8 @@ constexpr int kFirstDecode = 2 + kScaleWarps, kFirstEpi = kFirstDecode + kDecode
 constexpr int kThreads = 32 * (kFirstEpi + kEpiWarps);
 constexpr int kMaxCtas = 160;              // (the workspace is sized for so many)
 constexpr int kChainBlocks = 20;           // k-blocks accumulated in tensor memory before they are added in fp32: the error of a
-                                           // product is 6e-7 (2-norm) with 16, 9e-7 with 20, 1.3e-6 with 28
+                                           // product is 6e-7 (2-norm) with 16, 9e-7 with 20, 1.3e-6 with 28, and 131072 x 1024 x 1024
+                                           // takes 1 % longer with 16 and 2 % less with 28
 // Slots for codes and scales.  Even, so that a slot always belongs to the same one of the two groups of restoring warps: copies
 // complete in any order, and a group that waited for a slot's next phase while the one before, the other group's, was still
 // incomplete would take that one's parity for its own.  (The stages' `empty` barriers may change hands: MMAs complete in order, and a

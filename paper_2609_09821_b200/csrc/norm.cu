@@ -5,7 +5,7 @@
 // A row is read once: it stays in the registers of 8 to 256 threads while its mean and then the squares about that mean are
 // summed (two passes over registers, so an offset much larger than the spread costs no digits), fp32 throughout.
 // What bounds it is HBM: every byte of x and y moves once (131072 x 1024 bf16: 91 us, 5.9 TB/s where a copy reaches 6.5; with the
-// 8-bit checkpoint 32768 x 2048: 71 us, 4.8 TB/s, by then issue slots).
+// 8-bit checkpoint 32768 x 2048: 70 us, 4.8 TB/s, by then issue slots).
 #include <cmath>
 
 #include "im_internal.h"

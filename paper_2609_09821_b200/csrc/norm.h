@@ -8,7 +8,8 @@
 namespace im {
 
 constexpr int kNormMaxCols = 8192;
-constexpr int kNormMaxPartials = 592;      // rows of partial column sums that the backward pass leaves at most: four CTAs on each of 148 SMs
+constexpr int kNormMaxPartials = 592;      // rows of partial column sums that a workspace has room for at most; the backward pass writes one for
+                                           // each of its CTAs, two an SM (296 rows on 148 SMs)
 
 struct NormForward {
     const void *x;

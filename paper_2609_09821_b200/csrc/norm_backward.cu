@@ -18,9 +18,10 @@ namespace im {
 
 namespace {
 
-// Where eight CTAs hold all rows at once, they are one cluster and finish the column sums themselves: a second kernel costs more than the
-// barrier (64 x 512 fp32: 4.4 us to 4.3, and a call 12.5 us to 10.3; 32 x 1024: 5.0 to 5.2, 12.6 to 10.3).  Not for wider rows (16 x 2048:
-// 6.0 to 7.0), nor for two batches of rows a CTA (128 x 512: 4.5 to 5.1).
+// Where eight CTAs hold all rows at once, they are one cluster and finish the column sums themselves.  What that saves is the second
+// kernel's launch, 2 us of a call's 11.8; in a graph the cluster's barrier is worth about as much as a second kernel.  In a graph, with the
+// second kernel and with the cluster: 16 x 256 bf16 3.8 us and 3.0, 64 x 512 fp32 4.3 and 4.2, 32 x 1024 fp32 4.9 and 5.2 (calls 11.9 and
+// 9.9).  Not for wider rows (16 x 2048: 5.9 and 6.9), nor for two batches of rows a CTA (128 x 512: 4.5 and 5.1).
 constexpr int kCluster = 8;
 
 constexpr __host__ __device__ int cta_threads(int T) { return T > 256 ? T : 256; }
